@@ -257,6 +257,127 @@ int rosaq_pca_headwise(const void* X_dev, int32_t n_cal, int32_t D, int64_t ldx,
 int rosaq_pca_full(const void* X_dev, int32_t n_cal, int32_t D, int64_t ldx, float* Q_host,
                    double* eigenvalues_host, void* hip_stream);
 
+/* ---- the attention between the q/k/v projections and the output projection -------------------------------
+ *
+ * rosaq_linear_batch makes q, k and v of Eq. 5 and rosaq_linear_headwise takes the concatenated heads H_h of Eq. 6;
+ * what lies between runs in two calls: rosaq_cache_append turns q and k to their positions and writes k and v to a
+ * cache as 4- or 8-bit codes, rosaq_attention reads the cache.  Matrices are as there: fp16 [M x heads * head_dim], a row's
+ * heads side by side, row m at p + m * ld, 16-byte aligned, ld a multiple of 8.  All calls are asynchronous on hip_stream,
+ * allocate nothing, never synchronise and may be captured into a graph; the current device must be the one that holds
+ * the memory.  Outputs must not overlap inputs except where said.
+ *
+ * Integers in DEVICE memory are not seen by the host, so what they may hold is defined for every value: a slot, position or
+ * page outside its range means "none" (see each call), lengths are cut to the capacity.  Nothing is read or written through them. */
+
+/* Rotary positions: pair (a, b) of a head at position p becomes (a cos - b sin, b cos + a sin), cos and sin of p f_i in
+ * fp32 from a table, products and sums in fp64, rounded to fp32 and from there to fp16.  The pairs are channels (i, i + rot_dim/2)
+ * (HALF) or (2 i, 2 i + 1) (INTERLEAVED), i < rot_dim/2; channels from rot_dim on are kept.  f_i = base^(-2 i / rot_dim), and
+ *   LINEAR      f_i / factor
+ *   WAVELENGTH  with the turns t = trained_positions f_i / (2 pi) of the pair over the trained length: f_i where t >= high,
+ *               f_i / factor where t <= low, blended linearly in t between */
+#define ROSAQ_ROPE_HALF        0
+#define ROSAQ_ROPE_INTERLEAVED 1
+#define ROSAQ_ROPE_SCALE_NONE       0
+#define ROSAQ_ROPE_SCALE_LINEAR     1
+#define ROSAQ_ROPE_SCALE_WAVELENGTH 2
+
+typedef struct {
+  double base;               /* > 1                                                            */
+  int32_t rot_dim;           /* channels of a head that turn: a multiple of 16, at most 128    */
+  int32_t scaling;           /* ROSAQ_ROPE_SCALE_*                                              */
+  double factor;             /* LINEAR, WAVELENGTH: > 0                                         */
+  double low, high;          /* WAVELENGTH: 0 <= low < high, in turns                           */
+  double trained_positions;  /* WAVELENGTH: > 0                                                 */
+} rosaq_rope_desc;
+
+/* rosaq_rope_table - the angles of positions 0 .. positions - 1 (at most 2^24), computed in fp64 and rounded once:
+ * table_dev DEVICE fp32 [positions][rot_dim / 2][2] (cos, sin), 8-byte aligned.  Made once for as long as a model is
+ * served.  Errors: NULL, SHAPE, ARG, ALIGN, HIP. */
+int rosaq_rope_table(const rosaq_rope_desc* desc, void* table_dev, int32_t positions, void* hip_stream);
+
+/* How the calls below turn heads. */
+typedef struct {
+  const void* table;         /* DEVICE, from rosaq_rope_table or of that form                   */
+  int32_t positions;         /* rows of the table                                               */
+  int32_t rot_dim;           /* multiple of 16 in [16, head_dim]                                */
+  int32_t layout;            /* ROSAQ_ROPE_HALF / _INTERLEAVED                                  */
+} rosaq_rope_angles;
+
+/* rosaq_rope - y = x with every head turned to its row's position.  positions_dev DEVICE int32 [M]; a row whose position
+ * lies outside [0, positions) is left unwritten.  head_dim 64 or 128.  y may be x (same ld).
+ * Errors: NULL, SHAPE, ARG (head_dim, layout, partly overlapping y), ALIGN, HIP. */
+int rosaq_rope(const rosaq_rope_angles* rope, const int32_t* positions_dev, const void* x_dev, int32_t M, int64_t ldx,
+               int32_t heads, int32_t head_dim, void* y_dev, int64_t ldy, void* hip_stream);
+
+/* A cache of quantised keys and values: num_pages pages of page_tokens tokens, owned by the caller, who hands pages out
+ * to sequences.  Slot s is token s % page_tokens of page s / page_tokens. */
+typedef struct {
+  int32_t kv_heads;
+  int32_t head_dim;          /* 64 or 128                                                       */
+  int32_t bits;              /* 4 or 8                                                          */
+  int32_t page_tokens;       /* power of two in [16, 4096]                                      */
+  int32_t num_pages;
+  void* data;                /* DEVICE, rosaq_cache_bytes bytes, 256-byte aligned; need not be cleared */
+} rosaq_cache;
+
+/* Bytes of a cache's data; 0 where the shape is wrong (rosaq_last_error says why).  A token takes, for a head and for
+ * keys and values each, head_dim * bits / 8 bytes of codes and 4 bytes of scale and zero. */
+size_t rosaq_cache_bytes(int32_t kv_heads, int32_t head_dim, int32_t bits, int32_t page_tokens, int32_t num_pages);
+
+/* rosaq_cache_append - writes M tokens' keys and values to their slots, quantised per token and head with the quantiser of
+ * rosaq_pack_weights over a range that always holds zero (a group of one sign would lose its values otherwise):
+ *     lo = min(0, min x), hi = max(0, max x), top = 2^bits - 1, s = fp16(max((hi - lo) / top, 2^-14)), z = clamp(rne(-lo / s), 0, top),
+ *     t = floor(65504 / s), code = clamp(rne(x / s) + z, max(0, z - t), min(top, z + t)),  value (code - z) s
+ * (fp32 arithmetic; t keeps the value within fp16).  A head with NaN or Inf gets a NaN scale: all its channels read as NaN.
+ *   slots_dev  DEVICE int64 [M]; a token whose slot is none of the cache's is skipped.  The slots of a call must differ:
+ *              what two tokens leave in one slot is unspecified
+ *   k_dev, v_dev  DEVICE fp16 [M x kv_heads * head_dim]
+ *   rope       NULL, or how keys are turned first (and rounded to fp16); positions_dev DEVICE int32 [M], a token whose
+ *              position lies outside the table is skipped
+ *   q_dev      NULL, or queries [M x q_heads * head_dim] to turn in the same launch (rope not NULL) into q_out_dev, which may be
+ *              q_dev itself; rows of skipped tokens are left unwritten
+ * Errors: NULL, SHAPE, ARG, ALIGN, HIP. */
+int rosaq_cache_append(const rosaq_cache* cache, const int64_t* slots_dev, int32_t M, const void* k_dev, int64_t ldk,
+                       const void* v_dev, int64_t ldv, const rosaq_rope_angles* rope, const int32_t* positions_dev,
+                       const void* q_dev, int64_t ldq, int32_t q_heads, void* q_out_dev, int64_t ldq_out, void* hip_stream);
+
+/* rosaq_cache_read - the values of M slots (any order, any number of times) as fp16: (code - z) s rounded once.  k_dev or v_dev may be
+ * NULL; rows of slots that are none of the cache's are left unwritten.  Errors: NULL, SHAPE, ARG, ALIGN, HIP. */
+int rosaq_cache_read(const rosaq_cache* cache, const int64_t* slots_dev, int32_t M, void* k_dev, int64_t ldk, void* v_dev,
+                     int64_t ldv, void* hip_stream);
+
+/* rosaq_attention - y = softmax(scale q K^T) V for the rows of several sequences over their tokens in the cache:
+ * from one new token a sequence to whole prompts, with or without a prefix that all sequences share.
+ * Row i of a sequence of n rows and l cached tokens (the rows' own tokens among them, appended before) sees all of the prefix
+ * and, of the sequence's tokens, all (causal 0) or those below l - n + i + 1 (causal 1).  A row that sees nothing is zero.
+ * q_heads is a multiple of the cache's kv_heads: query head h reads kv head h / (q_heads / kv_heads).
+ * Scores, sums and the softmax's statistics are fp32, probabilities are rounded to fp16 for their product with the values, y once. */
+typedef struct {
+  const rosaq_cache* cache;
+  int32_t q_heads;
+  int32_t M;                        /* rows of q and y                                                  */
+  int32_t sequences;
+  int32_t max_rows;                 /* rows of a sequence: at most this many (further ones are left unwritten) */
+  int32_t max_kv;                   /* cached tokens of a sequence, without the prefix: at most this many (cut beyond) */
+  int32_t prefix_len;               /* tokens of the shared prefix, 0 for none                          */
+  int32_t causal;                   /* 0 or 1                                                           */
+  float scale;                      /* e.g. head_dim^-1/2                                               */
+  const void* q_dev; int64_t ldq;   /* DEVICE fp16 [M x q_heads * head_dim], turned already             */
+  void* y_dev; int64_t ldy;         /* DEVICE fp16 [M x q_heads * head_dim], apart from q; rows of no sequence stay as they are */
+  const int32_t* row_start_dev;     /* DEVICE int32 [sequences + 1], ascending: sequence b has rows row_start[b] .. row_start[b+1] - 1. */
+                                    /* NULL: sequence b has row b (max_rows 1)                          */
+  const int32_t* kv_len_dev;        /* DEVICE int32 [sequences]                                         */
+  const int32_t* pages_dev;         /* DEVICE int32 [sequences x page_stride]: pages of a sequence's tokens, in order.  Tokens of a */
+  int32_t page_stride;              /* page outside [0, num_pages) are seen by no row.  page_stride * page_tokens >= max_kv */
+  const int32_t* prefix_pages_dev;  /* DEVICE int32 [ceil(prefix_len / page_tokens)], NULL without a prefix */
+} rosaq_attention_desc;
+
+/* ws_dev: DEVICE scratch of rosaq_workspace_bytes_attention(desc) bytes, 256-byte aligned, needs no initialisation; the
+ * size depends on the cache's shape and the numbers of the first block of the struct alone (pointers may still be NULL).  Calls that share
+ * a workspace must not overlap in time.  Errors: NULL, SHAPE, ARG, ALIGN, WORKSPACE, HIP (workspace_bytes: 0 on any). */
+size_t rosaq_workspace_bytes_attention(const rosaq_attention_desc* desc);
+int rosaq_attention(const rosaq_attention_desc* desc, void* ws_dev, size_t ws_bytes, void* hip_stream);
+
 /* rosaq_stream_probe - measurement aid, no arithmetic of the method: one launch of
  * `workgroups` x `threads` in which every wave reads its own contiguous share of
  * src_dev (src_bytes in total, 1 KiB per load) and every workgroup then reads

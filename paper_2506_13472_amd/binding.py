@@ -13,6 +13,8 @@ import os
 import numpy as np
 
 Q_NONE, Q_FULL, Q_HEADWISE = 0, 1, 2
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_SCALE_NONE, ROPE_SCALE_LINEAR, ROPE_SCALE_WAVELENGTH = range(3)
 SELECT_TOP, SELECT_TOP_PER_HEAD, SELECT_BOTTOM, SELECT_CONSECUTIVE, SELECT_TOP_AND_BOTTOM = range(5)
 
 ERR_NAMES = {0: "OK", -1: "NULL", -2: "SHAPE", -3: "ARG", -4: "MODE", -5: "ALIGN",
@@ -24,6 +26,7 @@ LIB_PATH = os.environ.get("ROSAQ_LIB") or os.path.join(os.path.dirname(os.path.a
 EXPORTED = ["rosaq_pack_weights", "rosaq_workspace_bytes", "rosaq_workspace_bytes_batch", "rosaq_workspace_bytes_min", "rosaq_linear", "rosaq_linear_headwise",
             "rosaq_linear_headwise_static", "rosaq_linear_batch", "rosaq_linear_swiglu", "rosaq_mlp_swiglu", "rosaq_workspace_bytes_mlp", "rosaq_stream_probe", "rosaq_packed_clone", "rosaq_pca_headwise", "rosaq_pca_full",
             "rosaq_packed_info", "rosaq_packed_export", "rosaq_tune", "rosaq_launch_shape", "rosaq_launch_many_rows", "rosaq_block_map", "rosaq_packed_image", "rosaq_free",
+            "rosaq_cache_bytes", "rosaq_rope_table", "rosaq_rope", "rosaq_cache_append", "rosaq_cache_read", "rosaq_attention", "rosaq_workspace_bytes_attention",
             "rosaq_last_error"]
 
 
@@ -35,6 +38,28 @@ class PackDesc(C.Structure):
                 ("K", C.c_int32), ("bits", C.c_int32), ("group", C.c_int32),
                 ("select_rule", C.c_int32), ("host_only", C.c_int32), ("select_arg", C.c_int32),
                 ("rotation_absorbed", C.c_int32)]
+
+
+class RopeDesc(C.Structure):
+    _fields_ = [("base", C.c_double), ("rot_dim", C.c_int32), ("scaling", C.c_int32), ("factor", C.c_double),
+                ("low", C.c_double), ("high", C.c_double), ("trained_positions", C.c_double)]
+
+
+class RopeAngles(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("positions", C.c_int32), ("rot_dim", C.c_int32), ("layout", C.c_int32)]
+
+
+class Cache(C.Structure):
+    _fields_ = [("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("bits", C.c_int32), ("page_tokens", C.c_int32),
+                ("num_pages", C.c_int32), ("data", C.c_void_p)]
+
+
+class AttentionDesc(C.Structure):
+    _fields_ = [("cache", C.POINTER(Cache)), ("q_heads", C.c_int32), ("M", C.c_int32), ("sequences", C.c_int32),
+                ("max_rows", C.c_int32), ("max_kv", C.c_int32), ("prefix_len", C.c_int32), ("causal", C.c_int32),
+                ("scale", C.c_float), ("q", C.c_void_p), ("ldq", C.c_int64), ("y", C.c_void_p), ("ldy", C.c_int64),
+                ("row_start", C.c_void_p), ("kv_len", C.c_void_p), ("pages", C.c_void_p), ("page_stride", C.c_int32),
+                ("prefix_pages", C.c_void_p)]
 
 
 class RosaqError(RuntimeError):
@@ -104,6 +129,20 @@ def lib() -> C.CDLL:
         L.rosaq_packed_image.restype = C.c_int
         L.rosaq_block_map.argtypes = [i32, i32, i32, C.POINTER(i32), C.POINTER(i32)]
         L.rosaq_block_map.restype = C.c_int
+        L.rosaq_cache_bytes.argtypes = [i32] * 5
+        L.rosaq_cache_bytes.restype = sz
+        L.rosaq_rope_table.argtypes = [C.POINTER(RopeDesc), vp, i32, vp]
+        L.rosaq_rope_table.restype = C.c_int
+        L.rosaq_rope.argtypes = [C.POINTER(RopeAngles), vp, vp, i32, i64, i32, i32, vp, i64, vp]
+        L.rosaq_rope.restype = C.c_int
+        L.rosaq_cache_append.argtypes = [C.POINTER(Cache), vp, i32, vp, i64, vp, i64, C.POINTER(RopeAngles), vp, vp, i64, i32, vp, i64, vp]
+        L.rosaq_cache_append.restype = C.c_int
+        L.rosaq_cache_read.argtypes = [C.POINTER(Cache), vp, i32, vp, i64, vp, i64, vp]
+        L.rosaq_cache_read.restype = C.c_int
+        L.rosaq_workspace_bytes_attention.argtypes = [C.POINTER(AttentionDesc)]
+        L.rosaq_workspace_bytes_attention.restype = sz
+        L.rosaq_attention.argtypes = [C.POINTER(AttentionDesc), vp, sz, vp]
+        L.rosaq_attention.restype = C.c_int
         L.rosaq_free.argtypes = [vp]
         L.rosaq_free.restype = None
         L.rosaq_last_error.argtypes = []
@@ -262,6 +301,46 @@ def rosaq_pca_full(x_ptr: int, n_cal: int, D: int, ldx: int, stream: int = 0):
     lam = np.empty(max(D, 0), np.float64)
     _check(lib().rosaq_pca_full(x_ptr, n_cal, D, ldx, _ptr(Q), _ptr(lam), stream))
     return Q, lam
+
+
+def rosaq_cache_bytes(kv_heads: int, head_dim: int, bits: int, page_tokens: int, num_pages: int) -> int:
+    n = lib().rosaq_cache_bytes(kv_heads, head_dim, bits, page_tokens, num_pages)
+    if n == 0:
+        raise RosaqError(-2, rosaq_last_error())
+    return n
+
+
+def rosaq_rope_table(table_ptr: int, positions: int, rot_dim: int, base: float = 10000.0, scaling: int = ROPE_SCALE_NONE,
+                     factor: float = 1.0, low: float = 0.0, high: float = 0.0, trained_positions: float = 0.0, stream: int = 0):
+    d = RopeDesc(base, rot_dim, scaling, factor, low, high, trained_positions)
+    _check(lib().rosaq_rope_table(C.byref(d), table_ptr, positions, stream))
+
+
+def rosaq_rope(rope: RopeAngles, positions_ptr: int, x_ptr: int, M: int, ldx: int, heads: int, head_dim: int, y_ptr: int,
+               ldy: int, stream: int = 0):
+    _check(lib().rosaq_rope(rope, positions_ptr, x_ptr, M, ldx, heads, head_dim, y_ptr, ldy, stream))
+
+
+def rosaq_cache_append(cache: Cache, slots_ptr: int, M: int, k_ptr: int, ldk: int, v_ptr: int, ldv: int,
+                       rope: RopeAngles | None = None, positions_ptr: int = 0, q_ptr: int = 0, ldq: int = 0, q_heads: int = 0,
+                       q_out_ptr: int = 0, ldq_out: int = 0, stream: int = 0):
+    _check(lib().rosaq_cache_append(cache, slots_ptr, M, k_ptr, ldk, v_ptr, ldv, rope, positions_ptr, q_ptr, ldq, q_heads,
+                                    q_out_ptr, ldq_out, stream))
+
+
+def rosaq_cache_read(cache: Cache, slots_ptr: int, M: int, k_ptr: int, ldk: int, v_ptr: int, ldv: int, stream: int = 0):
+    _check(lib().rosaq_cache_read(cache, slots_ptr, M, k_ptr, ldk, v_ptr, ldv, stream))
+
+
+def rosaq_workspace_bytes_attention(desc: AttentionDesc) -> int:
+    n = lib().rosaq_workspace_bytes_attention(C.byref(desc))
+    if n == 0:
+        raise RosaqError(-2, rosaq_last_error())
+    return n
+
+
+def rosaq_attention(desc: AttentionDesc, ws_ptr: int, ws_bytes: int, stream: int = 0):
+    _check(lib().rosaq_attention(desc, ws_ptr, ws_bytes, stream))
 
 
 def rosaq_stream_probe(src_ptr: int, src_bytes: int, shared_ptr: int, shared_bytes: int,

@@ -13,9 +13,9 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "librosaq.so")
-HOST_SOURCES = ["rosaq_pack.cpp", "rosaq_api.cpp"]
+HOST_SOURCES = ["rosaq_pack.cpp", "rosaq_api.cpp", "rosaq_attention.cpp"]
 HIP_SOURCES = ["rosaq_kernels.hip", "rosaq_pca.hip", "rosaq_static.hip", "rosaq_quant.hip", "rosaq_rotate.hip",
-               "rosaq_wide.hip"]
+               "rosaq_wide.hip", "rosaq_cache.hip", "rosaq_attention.hip"]
 
 
 def hipcc() -> str:
