@@ -145,8 +145,7 @@ static int check_attention(const rosaq_attention_desc* d, AttendArgs* a, bool po
     if (!d->kv_len_dev) return fail(ROSAQ_ERR_NULL, "kv_len_dev is NULL");
     if (d->max_kv > 0 && !d->pages_dev) return fail(ROSAQ_ERR_NULL, "pages_dev is NULL");
     if (d->prefix_len > 0 && !d->prefix_pages_dev) return fail(ROSAQ_ERR_NULL, "prefix_pages_dev is NULL");
-    if (d->page_stride < 0 || static_cast<int64_t>(d->page_stride) * shape.page_tokens < d->max_kv)
-      return fail(ROSAQ_ERR_SHAPE, "page_stride x page_tokens is smaller than max_kv");
+    if (d->page_stride < 0) return fail(ROSAQ_ERR_SHAPE, "page_stride must not be negative");
     if (misaligned(d->kv_len_dev, 4) || misaligned(d->row_start_dev, 4) || misaligned(d->pages_dev, 4) || misaligned(d->prefix_pages_dev, 4))
       return fail(ROSAQ_ERR_ALIGN, "the integer arrays must be 4-byte aligned");
   }
@@ -155,7 +154,9 @@ static int check_attention(const rosaq_attention_desc* d, AttendArgs* a, bool po
   a->row_start = d->row_start_dev; a->kv_len = d->kv_len_dev;
   a->pages = d->pages_dev; a->page_stride = d->page_stride;
   a->prefix_pages = d->prefix_pages_dev; a->prefix_len = d->prefix_len;
-  a->max_rows = d->max_rows; a->max_kv = d->max_kv; a->causal = d->causal;
+  // a plan for max_kv tokens serves a table cut to the pages that are in use
+  const int64_t room = pointers ? static_cast<int64_t>(d->page_stride) * shape.page_tokens : d->max_kv;
+  a->max_rows = d->max_rows; a->max_kv = d->max_kv; a->capacity = static_cast<int>(room < d->max_kv ? room : d->max_kv); a->causal = d->causal;
   a->scale_log2 = static_cast<float>(static_cast<double>(d->scale) * 1.4426950408889634);
   a->dim = shape.head_dim; a->bits = shape.bits;
   a->part = nullptr;
@@ -262,7 +263,7 @@ int rosaq_attention(const rosaq_attention_desc* desc, void* ws_dev, size_t ws_by
   const int rc = check_attention(desc, &a, true);
   if (rc != ROSAQ_OK) return rc;
   const AttendPlan p = plan_attention(a);
-  if (p.grid >= kMaxGrid) return fail(ROSAQ_ERR_SHAPE, "sequences x max_rows x q_heads too large: split the call");
+  if (p.own.grid >= kMaxGrid || p.prefix.grid >= kMaxGrid) return fail(ROSAQ_ERR_SHAPE, "sequences x max_rows x q_heads too large: split the call");
   if (p.ws_bytes) {
     if (!ws_dev || ws_bytes < p.ws_bytes) return fail(ROSAQ_ERR_WORKSPACE, "workspace missing or too small");
     if (misaligned(ws_dev, 256)) return fail(ROSAQ_ERR_ALIGN, "workspace must be 256-byte aligned");

@@ -84,16 +84,29 @@ struct AttendArgs {
   const int32_t* pages; int64_t page_stride;
   const int32_t* prefix_pages; int prefix_len;
   int max_rows, max_kv;
+  int capacity;                             // tokens of a sequence that are looked at: of max_kv, those that `pages` has room for
   int causal;
   float scale_log2;                         // scale * log2(e)
   int dim, bits;
   float* part;                              // partial results (AttendPlan::parts > 1)
 };
-// How a call runs: the 32-token steps a workgroup takes, and the parts every row is computed in (1: stored directly).
-struct AttendPlan {
+// One launch of a call: the rows of every sequence over their own tokens, behind the prefix or not, or all rows of the call
+// over the prefix.
+enum AttendOver { kOwn, kPrefixAndOwn, kPrefix };
+struct AttendLaunch {
+  int over = kPrefixAndOwn;
+  int row_tiles = 0;        // 16-row tiles of a wave, 0: the kernel for up to 16 rows
+  int tiles = 1;            // workgroups that share the rows of a sequence and kv head
+  int steps = 0, parts = 1; // steps of kStep or kStage tokens that a workgroup takes; workgroups that share all of them
+  int first_part = 0;       // number of the first of them among the parts of a row
+  int by_xcd = 0;           // workgroups of one sequence and kv head on one XCD
   int64_t grid = 0;         // workgroups
-  int steps = 0;
-  int parts = 1;
+};
+// How a call runs.  Every row is computed in own.parts (+ prefix.parts) parts; one alone is stored directly, more go through
+// the workspace and are joined by another launch.
+struct AttendPlan {
+  AttendLaunch own, prefix; // prefix.grid 0: not apart
+  int parts = 1;            // of all launches
   size_t ws_bytes = 0;
 };
 AttendPlan plan_attention(const AttendArgs& a);
