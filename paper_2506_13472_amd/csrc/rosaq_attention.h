@@ -99,6 +99,7 @@ struct AttendLaunch {
   int tiles = 1;            // workgroups that share the rows of a sequence and kv head
   int steps = 0, parts = 1; // steps of kStep or kStage tokens that a workgroup takes; workgroups that share all of them
   int first_part = 0;       // number of the first of them among the parts of a row
+  int alone = 0;            // up to 16 rows: a wave takes all steps of its part, four of them a workgroup
   int by_xcd = 0;           // workgroups of one sequence and kv head on one XCD
   int64_t grid = 0;         // workgroups
 };

@@ -49,9 +49,9 @@ __device__ __forceinline__ int steps_of(const AttendArgs& a, int over, int step,
 // A workgroup's share of a launch.  Workgroups go to the XCDs in turn; with by_xcd, those of one sequence and kv head, which read
 // the same codes, stay on one XCD and its L2.  Tiles go from the last to the first, which under the causal mask is from the longest.
 struct Share { int seq, kv_head, tile, part; bool any; };
-__device__ __forceinline__ Share share_of(const AttendArgs& a, const AttendLaunch& n) {
+__device__ __forceinline__ Share share_of(const AttendArgs& a, const AttendLaunch& n, int id) {
   const int heads = a.cache.kv_heads, seqs = n.over == kPrefix ? 1 : a.seqs, each = n.tiles * n.parts;
-  int id = blockIdx.x, pair, rest;
+  int pair, rest;
   if (n.by_xcd) {
     pair = (id >> 3) / each * 8 + (id & 7);
     rest = (id >> 3) % each;
@@ -67,14 +67,6 @@ __device__ __forceinline__ Rows launch_rows(const AttendArgs& a, int over, int s
   if (over != kPrefix) return rows_of(a, seq);
   return Rows{0, a.row_start ? min(max(a.row_start[a.seqs], 0), a.M) : a.seqs};
 }
-
-// What a lane holds of one step: codes of two records and the scales and zeros it needs of them.
-template <int D, int BITS> struct Step {
-  static constexpr int kDwords = D / 4 * BITS / 32;     // of a lane, keys or values of one record: 2, 4 or 8
-  uint32_t k[2][kDwords], v[2][kDwords];
-  uint32_t k_own[2];        // scale | zero of the key token that the lane multiplies
-  uint4 k_sz[2], v_sz[2];   // of tokens 4 g .. 4 g + 3
-};
 
 // `place`: the lane's place among the 64 of a plane
 template <int N> __device__ __forceinline__ void load_codes(uint32_t (&to)[N], const char* plane0, int place) {
@@ -104,17 +96,17 @@ template <int BITS> __device__ __forceinline__ half8 key_factor(const uint32_t* 
   }
 }
 
-// Channel j (of a lane's D / 16) of two tokens of a record as values (code - z) s, rounded to fp16 as reading the cache rounds them.  `w`: the
-// lane's dwords, dword 2 i + t = unit i of the tokens 2 t and 2 t + 1.
-template <int BITS> __device__ __forceinline__ half2v value_pair(const uint32_t* w, int j, int t, half2v c_lo, half2v c_hi, half2v s) {
+// Channel j (of a lane's D / 16) of two tokens of a record, as whole numbers code - z.  `w`: the lane's dwords, dword 2 i + t = unit
+// i of the tokens 2 t and 2 t + 1.
+template <int BITS> __device__ __forceinline__ half2v value_pair(const uint32_t* w, int j, int t, half2v c_lo, half2v c_hi) {
   const half2v sixteenth = {(_Float16)0.0625f, (_Float16)0.0625f};
   if constexpr (BITS == 4) {
     const uint32_t d = w[2 * (j / 4) + t] >> (j % 4 / 2 * 8);
-    if (j % 2 == 0) return (as_h2(and_or<false>(d, 0x000f000fu, 0x64006400u)) + c_lo) * s;
-    return __builtin_elementwise_fma(as_h2(and_or<false>(d, 0x00f000f0u, 0x64006400u)), sixteenth, c_hi) * s;
+    if (j % 2 == 0) return as_h2(and_or<false>(d, 0x000f000fu, 0x64006400u)) + c_lo;
+    return __builtin_elementwise_fma(as_h2(and_or<false>(d, 0x00f000f0u, 0x64006400u)), sixteenth, c_hi);
   } else {
     const uint32_t d = w[2 * (j / 2) + t];
-    return (as_h2(__builtin_amdgcn_perm(0x64646464u, d, j % 2 == 0 ? 0x04020400u : 0x04030401u)) + c_lo) * s;
+    return as_h2(__builtin_amdgcn_perm(0x64646464u, d, j % 2 == 0 ? 0x04020400u : 0x04030401u)) + c_lo;
   }
 }
 
@@ -131,21 +123,67 @@ template <int D> struct Part {
       : sums(a.part), stats(reinterpret_cast<float2*>(a.part + static_cast<int64_t>(parts) * a.M * a.q_heads * D)) {}
 };
 
-template <int D, int BITS>
-__global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a, AttendLaunch n, int parts) {
+// The power of two above a scale | zero's scale: s < 2^exponent_of <= 2 s.  (Of 0 -14, of NaN 17.)
+__device__ __forceinline__ float exponent_of(uint32_t sz) { return static_cast<float>(static_cast<int>(sz >> 10 & 0x1fu) - 14); }
+
+// A lane's share of a row, channels 4 g U .. + 4 U - 1, to y or to the row's partial results.
+template <int D>
+__device__ __forceinline__ void store_row(const AttendArgs& a, const Part<D>& out, int parts, int part, int64_t token, int head, int g,
+                                          float ref, float l, const floatx4 (&sum)[D / 16]) {
+  constexpr int U = D / 16;
+  if (parts == 1) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    _Float16* y = static_cast<_Float16*>(a.y) + token * a.ldy + head * D + 4 * g * U;
+#pragma unroll
+    for (int e = 0; e < 4 * U / 8; ++e) {
+      half8 h;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h[i] = static_cast<_Float16>(sum[(8 * e + i) % U][(8 * e + i) / U] * inv);
+      reinterpret_cast<uint4*>(y)[e] = __builtin_bit_cast(uint4, h);
+    }
+  } else {
+    const int64_t at = (static_cast<int64_t>(part) * a.M + token) * a.q_heads + head;
+    float* y = out.sums + at * D + 4 * g * U;
+#pragma unroll
+    for (int e = 0; e < 4 * U / 4; ++e) {
+      floatx4 h;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) h[i] = sum[(4 * e + i) % U][(4 * e + i) / U];
+      reinterpret_cast<floatx4*>(y)[e] = h;
+    }
+    if (g == 0) out.stats[at] = make_float2(ref, l);
+  }
+}
+
+// What a lane holds of one step: codes of two records and the scales and zeros it needs of them.
+template <int D, int BITS> struct Step {
+  static constexpr int kDwords = D / 4 * BITS / 32;     // of a lane, keys or values of one record: 2, 4 or 8
+  uint32_t k[2][kDwords], v[2][kDwords];
+  uint32_t k_own[2];        // scale | zero of the key token that the lane multiplies
+  uint4 k_sz[2], v_sz[2];   // of tokens 4 g .. 4 g + 3
+  int hidden;               // which of the two records have no page
+};
+
+// Few rows.  A wave takes one tile of up to 16 rows, alone (SPLIT 1: four tiles a workgroup) or as one of the four of a workgroup that take its
+// steps in turn (SPLIT 4) and add up what they have in LDS.
+//
+// Values enter the product as the whole numbers code - z and their scale s in the other factor, P' = fp16(p s): one rounding for
+// a product of three numbers, and an operation less for each of the values, which with so few rows is where the time goes.  So
+// that P' is in fp16's range whatever the scales are, the reference is one of p s, not of p; the sum of p is fp32.
+template <int D, int BITS, int SPLIT>
+__global__ __launch_bounds__(64 * kWaves, D == 128 && BITS == 8 ? 2 : 3) void attend_kernel(AttendArgs a, AttendLaunch n, int parts) {
   constexpr int U = D / 16, KS = D / 32;
-  __shared__ float lds_sum[kWaves][kRows][D + 4];
-  __shared__ float lds_ref[kWaves][kRows], lds_l[kWaves][kRows];
+  constexpr int kRecord = cache_record_bytes(D, BITS), kCodes = cache_code_bytes(D, BITS);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
-  const Share w = share_of(a, n);
+  const Share w = share_of(a, n, SPLIT == 1 ? static_cast<int>(blockIdx.x) * kWaves + wave : static_cast<int>(blockIdx.x));
   if (!w.any) return;
   const int kv_head = w.kv_head, seq = w.seq, tile = w.tile;
   const Rows rows = rows_of(a, seq);
   const int used = min(rows.count, a.max_rows) * a.group;         // rows of this kv head: (token, query head of the group)
   if (tile * kRows >= used) return;
   const int tokens = own_tokens(a, seq);
-  const int last = (min(tile * kRows + kRows, used) - 1) / a.group;
+  const int first = tile * kRows / a.group, last = (min(tile * kRows + kRows, used) - 1) / a.group;
   const int prefix_steps = prefix_steps_of(a, n.over, kStep);
   const int all = steps_of(a, n.over, kStep, tokens, rows.count, last);
   const int begin = w.part * n.steps, end = min(begin + n.steps, all);
@@ -153,12 +191,13 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a, Atten
 
   // rows of the tile: (token, head) of this lane's column, clamped into the sequence's
   const int my = min(tile * kRows + r, used - 1);
-  const int my_token = my / a.group, my_head = kv_head * a.group + my % a.group;
-  const int limit = visible(a, tokens, rows.count, my_token);
+  const int my_token = my / a.group;
+  const int limit = visible(a, tokens, rows.count, my_token), least = visible(a, tokens, rows.count, first);
 
   half8 q[KS];
   {
-    const _Float16* src = static_cast<const _Float16*>(a.q) + static_cast<int64_t>(rows.start + my_token) * a.ldq + my_head * D + g * (D / 4);
+    const _Float16* src = static_cast<const _Float16*>(a.q) + static_cast<int64_t>(rows.start + my_token) * a.ldq +
+                          (kv_head * a.group + my % a.group) * D + g * (D / 4);
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       const half8 h = as_h8(reinterpret_cast<const uint4*>(src)[s]);
@@ -168,23 +207,22 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a, Atten
 
   const CacheDev& c = a.cache;
   const int block_shift = c.page_shift - 4;
-  constexpr int kRecord = cache_record_bytes(D, BITS), kCodes = cache_code_bytes(D, BITS);
   const char* head_base = c.base + kv_head * c.head_bytes;
+  const int32_t* own_pages = a.pages + static_cast<int64_t>(seq) * a.page_stride;
 
-  // loads a step; `hidden` says which of its records have no page
-  auto load = [&](int step, Step<D, BITS>& x, int& hidden) {
+  auto load = [&](int step, Step<D, BITS>& x) {
     const bool own = step >= prefix_steps;
     const int block0 = (own ? step - prefix_steps : step) * 2;
-    const int32_t* table = own ? a.pages + static_cast<int64_t>(seq) * a.page_stride : a.prefix_pages;
+    const int32_t* table = own ? own_pages : a.prefix_pages;
     const int blocks = ((own ? tokens : a.prefix_len) + kCacheBlock - 1) / kCacheBlock;
-    hidden = 0;
+    x.hidden = 0;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       const int block = block0 + b;
       int page = block < blocks ? table[block >> block_shift] : -1;
       page = __builtin_amdgcn_readfirstlane(page);
       const bool bad = page < 0 || page >= c.num_pages;
-      hidden |= bad ? 1 << b : 0;
+      x.hidden |= bad ? 1 << b : 0;
       // a record without a page is hidden below; the loads then take the cache's first one
       const char* rec = head_base + (bad ? 0 : page * c.page_bytes + static_cast<int64_t>(block & ((1 << block_shift) - 1)) * kRecord);
       load_codes(x.k[b], rec, r * 4 + g);
@@ -201,16 +239,11 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a, Atten
   for (int j = 0; j < U; ++j) sum[j] = floatx4{0.f, 0.f, 0.f, 0.f};
   float ref = kNoScore, l = 0.f;
 
-  for (int step = begin + wave; step < end; step += kWaves) {
-    Step<D, BITS> x;
-    int hidden;
-    load(step, x, hidden);
+  auto multiply = [&](int step, const Step<D, BITS>& x) {
     const bool own = step >= prefix_steps;
     const int t0 = (own ? step - prefix_steps : step) * kStep;
-    const int lim = (own ? limit : a.prefix_len) - t0;               // of the step's 32 tokens, this row sees those below it
-    const int held = (own ? tokens : a.prefix_len) - t0;             // and those below this are written at all
-
-    float score[2][4];
+    float score[8];
+    uint32_t v_sz[8], v_z[8];     // scales that the lane's row takes, zeros that its channels take: of the same tokens
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       const half2v own_sz = as_h2(x.k_own[b]);
@@ -218,17 +251,29 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a, Atten
       floatx4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int k = 0; k < KS; ++k) s = mfma16(key_factor<BITS>(&x.k[b][k * BITS / 4], c_lo, c_hi), q[k], s);
-      const uint32_t sz[4] = {x.k_sz[b].x, x.k_sz[b].y, x.k_sz[b].z, x.k_sz[b].w};
+      const uint32_t ks[4] = {x.k_sz[b].x, x.k_sz[b].y, x.k_sz[b].z, x.k_sz[b].w};
+      const uint32_t vs[4] = {x.v_sz[b].x, x.v_sz[b].y, x.v_sz[b].z, x.v_sz[b].w};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float scale = static_cast<float>(as_h2(sz[i]).x) * a.scale_log2;
-        const bool seen = b * kCacheBlock + 4 * g + i < lim && !(hidden >> b & 1);
-        score[b][i] = seen ? s[i] * scale : -INFINITY;
+        score[4 * b + i] = s[i] * (static_cast<float>(as_h2(ks[i]).x) * a.scale_log2);
+        v_sz[4 * b + i] = v_z[4 * b + i] = vs[i];
       }
     }
-    float most = score[0][0];
+    if (x.hidden != 0 || t0 + kStep > (own ? least : a.prefix_len)) {
+      // what a row does not see weighs nothing, and what no one has written may be NaN: its scale and zero are not used either
+      const int lim = (own ? limit : a.prefix_len) - t0 - 4 * g, held = (own ? tokens : a.prefix_len) - t0 - 4 * g;
 #pragma unroll
-    for (int i = 1; i < 8; ++i) most = fmaxf(most, score[i / 4][i % 4]);
+      for (int i = 0; i < 8; ++i) {
+        const int at = i / 4 * kCacheBlock + i % 4;
+        const bool there = !(x.hidden >> (i / 4) & 1);
+        score[i] = there && at < lim ? score[i] : -INFINITY;
+        v_sz[i] = there && at < lim ? v_sz[i] : 0u;
+        v_z[i] = there && at < held ? v_z[i] : 0u;
+      }
+    }
+    float most = score[0] + exponent_of(v_sz[0]);
+#pragma unroll
+    for (int i = 1; i < 8; ++i) most = fmaxf(most, score[i] + exponent_of(v_sz[i]));
     if (__any(most > ref + kRoom)) {
       most = fmaxf(most, __shfl_xor(most, 16, 64));
       most = fmaxf(most, __shfl_xor(most, 32, 64));
@@ -242,90 +287,92 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a, Atten
     half8 p;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      p[i] = static_cast<_Float16>(__builtin_amdgcn_exp2f(score[i / 4][i % 4] - ref));
-      l += static_cast<float>(p[i]);            // what the product below adds up, so that its rounding cancels
+      const float e = __builtin_amdgcn_exp2f(score[i] - ref);
+      l += e;
+      p[i] = static_cast<_Float16>(e * static_cast<float>(as_h2(v_sz[i]).x));
     }
-    half2v s2[2][2], c_lo[2][2], c_hi[2][2];
-    uint32_t worst = 0;
+    half2v c_lo[4], c_hi[4];
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const uint32_t sz[4] = {x.v_sz[b].x, x.v_sz[b].y, x.v_sz[b].z, x.v_sz[b].w};
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        half2v pair[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          // what no one has written may be NaN, and 0 x NaN is not 0
-          const bool there = b * kCacheBlock + 4 * g + 2 * t + e < held && !(hidden >> b & 1);
-          pair[e] = as_h2(there ? sz[2 * t + e] : 0u);
-          worst = max(worst, __builtin_bit_cast(uint32_t, pair[e]) & 0x7fffu);
-        }
-        s2[b][t] = half2v{pair[0].x, pair[1].x};
-        const half2v z = {pair[0].y, pair[1].y};
-        c_lo[b][t] = minus(1024.f, z);
-        c_hi[b][t] = minus(64.f, z);
-      }
-    }
-    // A value that is NaN belongs to the rows that see it and to no other, but 0 x NaN is NaN: it goes to their sums of
-    // probabilities, and into the product as zero.
-    if (__any(worst >= 0x7c00u)) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const _Float16 s = s2[i / 4][i % 4 / 2][i % 2];
-        if ((__builtin_bit_cast(uint16_t, s) & 0x7c00u) != 0x7c00u) continue;
-        s2[i / 4][i % 4 / 2][i % 2] = (_Float16)0.f;
-        if (i / 4 * kCacheBlock + 4 * g + i % 4 < lim) l = NAN;
-      }
+    for (int t = 0; t < 4; ++t) {
+      const half2v z = {as_h2(v_z[2 * t]).y, as_h2(v_z[2 * t + 1]).y};
+      c_lo[t] = minus(1024.f, z);
+      c_hi[t] = minus(64.f, z);
     }
 #pragma unroll
     for (int j = 0; j < U; ++j) {
       half2v v[4];
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int t = 0; t < 2; ++t) v[2 * b + t] = value_pair<BITS>(x.v[b], j, t, c_lo[b][t], c_hi[b][t], s2[b][t]);
+      for (int t = 0; t < 4; ++t) v[t] = value_pair<BITS>(x.v[t / 2], j, t % 2, c_lo[t], c_hi[t]);
       const half8 f = {v[0].x, v[0].y, v[1].x, v[1].y, v[2].x, v[2].y, v[3].x, v[3].y};
       sum[j] = mfma16(f, p, sum[j]);
     }
-  }
+  };
 
-  // the waves' shares, brought to one reference and added
+  constexpr int kTurn = SPLIT == 1 ? 1 : kWaves;
+  int step = begin + (SPLIT == 1 ? 0 : wave);
+  if (step < end) {
+    // two steps' codes: one is multiplied while the next is on its way
+    Step<D, BITS> x, y;
+    load(step, x);
+    while (true) {
+      if (step + kTurn < end) load(step + kTurn, y);
+      multiply(step, x);
+      step += kTurn;
+      if (step >= end) break;
+      if (step + kTurn < end) load(step + kTurn, x);
+      multiply(step, y);
+      step += kTurn;
+      if (step >= end) break;
+    }
+  }
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
-  if (g == 0) { lds_ref[wave][r] = ref; lds_l[wave][r] = l; }
-  __syncthreads();
-  float top = lds_ref[0][r];
-#pragma unroll
-  for (int o = 1; o < kWaves; ++o) top = fmaxf(top, lds_ref[o][r]);
-  const float down = __builtin_amdgcn_exp2f(ref - top);
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < U; ++j) lds_sum[wave][r][(4 * g + i) * U + j] = sum[j][i] * down;
-  __syncthreads();
   const Part<D> out(a, parts);
-  for (int e = threadIdx.x; e < kRows * D / 2; e += 64 * kWaves) {
-    const int row = e / (D / 2), ch = e % (D / 2) * 2, at_row = tile * kRows + row;
-    if (at_row >= used) break;
-    float t = lds_ref[0][row], total = 0.f, y0 = 0.f, y1 = 0.f;
+  const int part = n.first_part + w.part;
+
+  if constexpr (SPLIT == 1) {
+    if (tile * kRows + r < used)
+      store_row<D>(a, out, parts, part, rows.start + my_token, kv_head * a.group + my % a.group, g, ref, l, sum);
+  } else {
+    // the waves' shares, brought to one reference and added
+    __shared__ float lds_sum[kWaves][kRows][D + 4];
+    __shared__ float lds_ref[kWaves][kRows], lds_l[kWaves][kRows];
+    if (g == 0) { lds_ref[wave][r] = ref; lds_l[wave][r] = l; }
+    __syncthreads();
+    float top = lds_ref[0][r];
 #pragma unroll
-    for (int o = 1; o < kWaves; ++o) t = fmaxf(t, lds_ref[o][row]);
+    for (int o = 1; o < kWaves; ++o) top = fmaxf(top, lds_ref[o][r]);
+    const float down = __builtin_amdgcn_exp2f(ref - top);
+    if (tile * kRows + r < used) {
 #pragma unroll
-    for (int o = 0; o < kWaves; ++o) {
-      total += lds_l[o][row] * __builtin_amdgcn_exp2f(lds_ref[o][row] - t);
-      y0 += lds_sum[o][row][ch];
-      y1 += lds_sum[o][row][ch + 1];
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < U; ++j) lds_sum[wave][r][(4 * g + i) * U + j] = sum[j][i] * down;
     }
-    const int64_t token = rows.start + at_row / a.group;
-    const int head = kv_head * a.group + at_row % a.group;
-    if (parts == 1) {
-      const float inv = total == 0.f ? 0.f : 1.f / total;
-      *reinterpret_cast<half2v*>(static_cast<_Float16*>(a.y) + token * a.ldy + head * D + ch) =
-          half2v{static_cast<_Float16>(y0 * inv), static_cast<_Float16>(y1 * inv)};
-    } else {
-      const int64_t at = (static_cast<int64_t>(n.first_part + w.part) * a.M + token) * a.q_heads + head;
-      *reinterpret_cast<float2*>(out.sums + at * D + ch) = make_float2(y0, y1);
-      if (ch == 0) out.stats[at] = make_float2(t, total);
+    __syncthreads();
+    for (int e = threadIdx.x; e < kRows * D / 2; e += 64 * kWaves) {
+      const int row = e / (D / 2), ch = e % (D / 2) * 2, at_row = tile * kRows + row;
+      if (at_row >= used) break;
+      float t = lds_ref[0][row], total = 0.f, y0 = 0.f, y1 = 0.f;
+#pragma unroll
+      for (int o = 1; o < kWaves; ++o) t = fmaxf(t, lds_ref[o][row]);
+#pragma unroll
+      for (int o = 0; o < kWaves; ++o) {
+        total += lds_l[o][row] * __builtin_amdgcn_exp2f(lds_ref[o][row] - t);
+        y0 += lds_sum[o][row][ch];
+        y1 += lds_sum[o][row][ch + 1];
+      }
+      const int64_t token = rows.start + at_row / a.group;
+      const int head = kv_head * a.group + at_row % a.group;
+      if (parts == 1) {
+        const float inv = total == 0.f ? 0.f : 1.f / total;
+        *reinterpret_cast<half2v*>(static_cast<_Float16*>(a.y) + token * a.ldy + head * D + ch) =
+            half2v{static_cast<_Float16>(y0 * inv), static_cast<_Float16>(y1 * inv)};
+      } else {
+        const int64_t at = (static_cast<int64_t>(part) * a.M + token) * a.q_heads + head;
+        *reinterpret_cast<float2*>(out.sums + at * D + ch) = make_float2(y0, y1);
+        if (ch == 0) out.stats[at] = make_float2(t, total);
+      }
     }
   }
 }
@@ -334,8 +381,10 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a, Atten
 //
 // A workgroup of four waves takes 64 RT query rows of one sequence and kv head (of all rows of the call, over the prefix) and
 // stages of 64 tokens.  The codes become fp16 factors once a stage, a record's keys and half of two records' values a wave, and go to LDS as whole MFMA
-// operands (1 KiB, lane order), which all waves read; two stages' worth of LDS, so that one barrier a stage is enough.  Keys are multiplied as the whole numbers
-// code - z and their scale acts on the scores, in fp32.  The sum of the probabilities is one more MFMA, against ones.
+// operands (1 KiB, lane order), which all waves read; two stages' worth of LDS, so that one barrier a stage is enough.
+// Keys are multiplied as the whole numbers code - z and their scale acts on the scores, in fp32: rounded factors would be off by
+// 2^-11 of a score that may be in the hundreds.  Values are (code - z) s, rounded as reading the cache rounds them.  The sum of the
+// probabilities is one more MFMA, against ones.
 constexpr int kStage = 4 * kCacheBlock;
 
 template <int D, int BITS> struct StageCodes {
@@ -344,6 +393,7 @@ template <int D, int BITS> struct StageCodes {
   uint32_t k[kKey], v[2][2 * kUnits];
   uint32_t k_own, v_own;      // scale | zero of the token the lane multiplies
   uint4 v_sz[2];
+  int hidden;                 // which of the stage's four records have no page
 };
 
 template <int D> struct alignas(16) StageLds {
@@ -367,7 +417,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
   __shared__ StageLds<D> lds[2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
-  const Share w = share_of(a, n);
+  const Share w = share_of(a, n, blockIdx.x);
   if (!w.any) return;
   const Rows rows = launch_rows(a, n.over, w.seq);
   const int used = (n.over == kPrefix ? rows.count : min(rows.count, a.max_rows)) * a.group;
@@ -402,81 +452,100 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
   const CacheDev& c = a.cache;
   const int block_shift = c.page_shift - 4;
   const char* head_base = c.base + w.kv_head * c.head_bytes;
+  const int32_t* own_pages = a.pages + static_cast<int64_t>(w.seq) * a.page_stride;
+  // of a lane: its codes within a record
+  constexpr int kAllUnits = D / 16 * BITS / 16;
+  const uint32_t k_at = (r * 4 + g) * (Codes::kKey == 2 ? 8 : 16);
+  const uint32_t v_at = kCodes + (kAllUnits == 4 ? (wave & 1) * 1024 + lane * 16 : (kAllUnits == 2 ? lane * 16 + (wave & 1) * 8 : lane * 8));
 
-  // loads this wave's share of a stage; `hidden`: which of the stage's four records have no page
-  auto load = [&](int stage, Codes& x, int& hidden) {
+  // pages of a stage's records (-1: none), a stage ahead of their use
+  auto look_up = [&](int stage, int (&page)[4]) {
     const bool own = stage >= prefix_stages;
     const int block0 = (own ? stage - prefix_stages : stage) * 4;
-    const int32_t* table = own ? a.pages + static_cast<int64_t>(w.seq) * a.page_stride : a.prefix_pages;
+    const int32_t* table = own ? own_pages : a.prefix_pages;
     const int blocks = ((own ? tokens : a.prefix_len) + kCacheBlock - 1) / kCacheBlock;
-    const char* rec[4];
-    hidden = 0;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) page[b] = stage < end && block0 + b < blocks ? table[(block0 + b) >> block_shift] : -1;
+  };
+  // loads this wave's share of a stage
+  auto load = [&](int stage, const int (&pages)[4], Codes& x) {
+    const int block0 = (stage >= prefix_stages ? stage - prefix_stages : stage) * 4;
+    int64_t at[4];
+    x.hidden = 0;
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
-      const int block = block0 + b;
-      int page = block < blocks ? table[block >> block_shift] : -1;
-      page = __builtin_amdgcn_readfirstlane(page);
+      const int page = __builtin_amdgcn_readfirstlane(pages[b]);
       const bool bad = page < 0 || page >= c.num_pages;
-      hidden |= bad ? 1 << b : 0;
-      rec[b] = head_base + (bad ? 0 : page * c.page_bytes + static_cast<int64_t>(block & ((1 << block_shift) - 1)) * kRecord);
+      x.hidden |= bad ? 1 << b : 0;
+      at[b] = bad ? 0 : page * c.page_bytes + static_cast<int64_t>((block0 + b) & ((1 << block_shift) - 1)) * kRecord;
     }
-    const char* mine = wave == 0 ? rec[0] : (wave == 1 ? rec[1] : (wave == 2 ? rec[2] : rec[3]));
-    load_codes(x.k, mine, r * 4 + g);
-    const uint32_t* sz = reinterpret_cast<const uint32_t*>(mine + 2 * kCodes);
-    x.k_own = sz[r];
-    x.v_own = sz[kCacheBlock + r];
+    const int64_t pair[2] = {wave < 2 ? at[0] : at[2], wave < 2 ? at[1] : at[3]};
+    const char* mine = head_base + (wave & 1 ? pair[1] : pair[0]);
+#pragma unroll
+    for (int p = 0; p < (Codes::kKey + 3) / 4; ++p) {
+      if constexpr (Codes::kKey == 2) {
+        const uint2 t = *reinterpret_cast<const uint2*>(mine + k_at);
+        x.k[0] = t.x; x.k[1] = t.y;
+      } else {
+        const uint4 t = *reinterpret_cast<const uint4*>(mine + k_at + p * 1024);
+        x.k[4 * p] = t.x; x.k[4 * p + 1] = t.y; x.k[4 * p + 2] = t.z; x.k[4 * p + 3] = t.w;
+      }
+    }
+    x.k_own = *reinterpret_cast<const uint32_t*>(mine + 2 * kCodes + 4u * r);
+    x.v_own = *reinterpret_cast<const uint32_t*>(mine + 2 * kCodes + kCacheBlock * 4 + 4u * r);
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      const char* of = wave < 2 ? rec[b] : rec[2 + b];
-      // the lane's units of channels (wave & 1) * U / 2 .. + U / 2 - 1
-      constexpr int all_units = D / 16 * BITS / 16;
-      const int half = wave & 1;
-      const char* at = of + kCodes + (all_units == 4 ? half * 1024 + lane * 16 : (all_units == 2 ? lane * 16 + half * 8 : lane * 8));
+      const char* of = head_base + pair[b];
       if constexpr (Codes::kUnits == 2) {
-        const uint4 v = *reinterpret_cast<const uint4*>(at);
+        const uint4 v = *reinterpret_cast<const uint4*>(of + v_at);
         x.v[b][0] = v.x; x.v[b][1] = v.y; x.v[b][2] = v.z; x.v[b][3] = v.w;
       } else {
-        const uint2 v = *reinterpret_cast<const uint2*>(at);
+        const uint2 v = *reinterpret_cast<const uint2*>(of + v_at);
         x.v[b][0] = v.x; x.v[b][1] = v.y;
       }
-      x.v_sz[b] = reinterpret_cast<const uint4*>(of + 2 * kCodes)[4 + g];
+      x.v_sz[b] = *reinterpret_cast<const uint4*>(of + 2 * kCodes + kCacheBlock * 4 + 16u * g);
     }
   };
 
   // codes -> factors in LDS
-  auto store = [&](int stage, const Codes& x, int hidden, StageLds<D>& to) {
+  auto store = [&](int stage, const Codes& x, StageLds<D>& to) {
     const bool own = stage >= prefix_stages;
     const int t0 = (own ? stage - prefix_stages : stage) * kStage;
     const int held = (own ? tokens : a.prefix_len) - t0;
     const half2v own_sz = as_h2(x.k_own);
     const half2v z = {own_sz.y, own_sz.y}, k_lo = minus(1024.f, z), k_hi = minus(64.f, z);
+    // a value that is NaN reaches the rows that see it through their scores (the product has zero for it)
+    if (g == 0) to.scale[wave * kCacheBlock + r] = (x.v_own & 0x7c00u) == 0x7c00u ? NAN : static_cast<float>(own_sz.x) * a.scale_log2;
 #pragma unroll
-    for (int s = 0; s < KS; ++s) to.k[wave][s][lane] = __builtin_bit_cast(uint4, key_factor<BITS>(&x.k[s * BITS / 4], k_lo, k_hi));
-    if (g == 0) {
-      // a value that is NaN reaches the rows that see it through their scores (the product has zero for it)
-      const bool odd = (x.v_own & 0x7c00u) == 0x7c00u;
-      to.scale[wave * kCacheBlock + r] = odd ? NAN : static_cast<float>(own_sz.x) * a.scale_log2;
+    for (int s = 0; s < KS; ++s)
+      to.k[wave][s][lane] = __builtin_bit_cast(uint4, key_factor<BITS>(&x.k[s * BITS / 4], k_lo, k_hi));
+    uint32_t sz[2][4];
+    uint32_t odd = 0;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      sz[b][0] = x.v_sz[b].x; sz[b][1] = x.v_sz[b].y; sz[b][2] = x.v_sz[b].z; sz[b][3] = x.v_sz[b].w;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) odd = max(odd, sz[b][i] & 0x7c00u);
+    }
+    if (held < kStage || x.hidden || __any(odd == 0x7c00u)) {       // NaN, written or never written, would make NaN of 0
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const int record = (wave & 2) + b;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (record * kCacheBlock + 4 * g + i >= held || (x.hidden >> record & 1) || (sz[b][i] & 0x7c00u) == 0x7c00u) sz[b][i] = 0u;
+      }
     }
     half2v s2[2][2], c_lo[2][2], c_hi[2][2];
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const int record = (wave & 2) + b;
-      const uint32_t sz[4] = {x.v_sz[b].x, x.v_sz[b].y, x.v_sz[b].z, x.v_sz[b].w};
+    for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        half2v pair[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const bool there = record * kCacheBlock + 4 * g + 2 * t + e < held && !(hidden >> record & 1) &&
-                             (sz[2 * t + e] & 0x7c00u) != 0x7c00u;
-          pair[e] = as_h2(there ? sz[2 * t + e] : 0u);
-        }
-        s2[b][t] = half2v{pair[0].x, pair[1].x};
-        const half2v vz = {pair[0].y, pair[1].y};
+        s2[b][t] = as_h2(__builtin_amdgcn_perm(sz[b][2 * t + 1], sz[b][2 * t], 0x05040100u));
+        const half2v vz = as_h2(__builtin_amdgcn_perm(sz[b][2 * t + 1], sz[b][2 * t], 0x07060302u));
         c_lo[b][t] = minus(1024.f, vz);
         c_hi[b][t] = minus(64.f, vz);
       }
-    }
 #pragma unroll
     for (int j = 0; j < U / 2; ++j) {
       half2v v[4];
@@ -486,9 +555,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
         for (int t = 0; t < 2; ++t) {
           if constexpr (D == 64 && BITS == 4) {      // one unit holds all four channels
             const uint32_t mine[2] = {x.v[b][0] >> ((wave & 1) * 8), x.v[b][1] >> ((wave & 1) * 8)};
-            v[2 * b + t] = value_pair<BITS>(mine, j, t, c_lo[b][t], c_hi[b][t], s2[b][t]);
+            v[2 * b + t] = value_pair<BITS>(mine, j, t, c_lo[b][t], c_hi[b][t]) * s2[b][t];
           } else {
-            v[2 * b + t] = value_pair<BITS>(x.v[b], j, t, c_lo[b][t], c_hi[b][t], s2[b][t]);
+            v[2 * b + t] = value_pair<BITS>(x.v[b], j, t, c_lo[b][t], c_hi[b][t]) * s2[b][t];
           }
         }
       const half8 f = {v[0].x, v[0].y, v[1].x, v[1].y, v[2].x, v[2].y, v[3].x, v[3].y};
@@ -513,69 +582,77 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
     const int t0 = (own ? stage - prefix_stages : stage) * kStage;
     if (own && t0 >= most_seen) return;
     const bool masked = hidden != 0 || t0 + kStage > (own ? least : a.prefix_len);
+    floatx4 score[4][RT];
 #pragma unroll
-    for (int p = 0; p < 2; ++p) {
-      floatx4 score[2][RT];
+    for (int s = 0; s < KS; ++s)         // a product never waits for the sum of the one before
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
+      for (int b = 0; b < 4; ++b) {
+        const half8 f = as_h8(from.k[b][s][lane]);
 #pragma unroll
-        for (int t = 0; t < RT; ++t) score[b][t] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-          const half8 f = as_h8(from.k[2 * p + b][s][lane]);
-#pragma unroll
-          for (int t = 0; t < RT; ++t) score[b][t] = mfma16(f, q[t][s], score[b][t]);
-        }
-        const floatx4 scale = *reinterpret_cast<const floatx4*>(&from.scale[(2 * p + b) * kCacheBlock + 4 * g]);
-#pragma unroll
-        for (int t = 0; t < RT; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) score[b][t][i] *= scale[i];
-        if (masked) {
-#pragma unroll
-          for (int t = 0; t < RT; ++t) {
-            const int lim = (own ? limit[t] : a.prefix_len) - t0 - (2 * p + b) * kCacheBlock - 4 * g;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) score[b][t][i] = i < lim && !(hidden >> (2 * p + b) & 1) ? score[b][t][i] : -INFINITY;
-          }
-        }
+        for (int t = 0; t < RT; ++t) score[b][t] = mfma16(f, q[t][s], s ? score[b][t] : floatx4{0.f, 0.f, 0.f, 0.f});
       }
-      float most[RT];
-      bool over = false;
 #pragma unroll
-      for (int t = 0; t < RT; ++t) {
-        most[t] = score[0][t][0];
+    for (int b = 0; b < 4; ++b) {
+      const floatx4 scale = *reinterpret_cast<const floatx4*>(&from.scale[b * kCacheBlock + 4 * g]);
 #pragma unroll
-        for (int i = 1; i < 8; ++i) most[t] = fmaxf(most[t], score[i / 4][t][i % 4]);
-        over |= most[t] > ref[t] + kRoom;
-      }
-      if (__any(over)) {
+      for (int t = 0; t < RT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) score[b][t][i] *= scale[i];
+    }
+    if (masked) {
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
-          most[t] = fmaxf(most[t], __shfl_xor(most[t], 16, 64));
-          most[t] = fmaxf(most[t], __shfl_xor(most[t], 32, 64));
-          const float next = fmaxf(ref[t], most[t] - kLead);
-          const float down = __builtin_amdgcn_exp2f(ref[t] - next);
-          l[t] *= floatx4{down, down, down, down};
+          const int lim = (own ? limit[t] : a.prefix_len) - t0 - b * kCacheBlock - 4 * g;
 #pragma unroll
-          for (int j = 0; j < U; ++j) sum[t][j] *= floatx4{down, down, down, down};
-          ref[t] = next;
+          for (int i = 0; i < 4; ++i) score[b][t][i] = i < lim && !(hidden >> b & 1) ? score[b][t][i] : -INFINITY;
         }
+    }
+    uint4 ahead[U];                    // the first two records' values, on their way while the probabilities are made
+#pragma unroll
+    for (int j = 0; j < U; ++j) ahead[j] = from.v[0][j][lane];
+    float most[RT];
+    bool over = false;
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      most[t] = score[0][t][0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) most[t] = fmaxf(most[t], score[i / 4][t][i % 4]);
+      over |= most[t] > ref[t] + kRoom;
+    }
+    if (__any(over)) {
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        most[t] = fmaxf(most[t], __shfl_xor(most[t], 16, 64));
+        most[t] = fmaxf(most[t], __shfl_xor(most[t], 32, 64));
+        const float next = fmaxf(ref[t], most[t] - kLead);
+        const float down = __builtin_amdgcn_exp2f(ref[t] - next);
+        l[t] *= floatx4{down, down, down, down};
+#pragma unroll
+        for (int j = 0; j < U; ++j) sum[t][j] *= floatx4{down, down, down, down};
+        ref[t] = next;
       }
+    }
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
       half8 prob[RT];
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
         uint32_t pk[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          pk[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(__builtin_amdgcn_exp2f(score[i / 2][t][i % 2 * 2] - ref[t]),
-                                                                        __builtin_amdgcn_exp2f(score[i / 2][t][i % 2 * 2 + 1] - ref[t])));
+        for (int i = 0; i < 4; ++i) {
+          const floatx4& x = score[2 * p + i / 2][t];
+          const int e = i % 2 * 2;
+          pk[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(
+              __builtin_amdgcn_exp2f(x[e] - ref[t]), __builtin_amdgcn_exp2f(x[e + 1] - ref[t])));
+        }
         prob[t] = as_h8(uint4{pk[0], pk[1], pk[2], pk[3]});
         l[t] = mfma16(ones, prob[t], l[t]);
       }
 #pragma unroll
       for (int j = 0; j < U; ++j) {
-        const half8 f = as_h8(from.v[p][j][lane]);
+        const half8 f = as_h8(p == 0 ? ahead[j] : from.v[1][j][lane]);
 #pragma unroll
         for (int t = 0; t < RT; ++t) sum[t][j] = mfma16(f, prob[t], sum[t][j]);
       }
@@ -584,15 +661,21 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
 
   if (begin < end) {
     Codes x;
-    int hidden, next_hidden = 0;
-    load(begin, x, hidden);
-    store(begin, x, hidden, lds[0]);
+    int page[4], hidden;
+    look_up(begin, page);
+    load(begin, page, x);
+    look_up(begin + 1, page);
+    store(begin, x, lds[0]);
+    hidden = x.hidden;
     lds_barrier();
     for (int stage = begin, cur = 0; stage < end; ++stage, cur ^= 1) {
-      if (stage + 1 < end) load(stage + 1, x, next_hidden);
+      if (stage + 1 < end) {
+        load(stage + 1, page, x);
+        look_up(stage + 2, page);
+      }
       if (!idle) multiply(stage, hidden, lds[cur]);
-      if (stage + 1 < end) store(stage + 1, x, next_hidden, lds[cur ^ 1]);
-      hidden = next_hidden;
+      if (stage + 1 < end) store(stage + 1, x, lds[cur ^ 1]);
+      hidden = x.hidden;
       lds_barrier();
     }
   }
@@ -602,38 +685,19 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
   for (int t = 0; t < RT; ++t) {
     const int my = first_row + 16 * t + r;
     if (my >= used) continue;
-    const int64_t token = rows.start + my / a.group;
-    const int head = w.kv_head * a.group + my % a.group;
-    if (parts == 1) {
-      const float inv = l[t][0] == 0.f ? 0.f : 1.f / l[t][0];
-      _Float16* y = static_cast<_Float16*>(a.y) + token * a.ldy + head * D + 4 * g * U;
-#pragma unroll
-      for (int e = 0; e < 4 * U / 8; ++e) {
-        half8 h;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) h[i] = static_cast<_Float16>(sum[t][(8 * e + i) % U][(8 * e + i) / U] * inv);
-        reinterpret_cast<uint4*>(y)[e] = __builtin_bit_cast(uint4, h);
-      }
-    } else {
-      const int64_t at = (static_cast<int64_t>(n.first_part + w.part) * a.M + token) * a.q_heads + head;
-      float* y = out.sums + at * D + 4 * g * U;
-#pragma unroll
-      for (int e = 0; e < 4 * U / 4; ++e) {
-        floatx4 h;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) h[i] = sum[t][(4 * e + i) % U][(4 * e + i) / U];
-        reinterpret_cast<floatx4*>(y)[e] = h;
-      }
-      if (g == 0) out.stats[at] = make_float2(ref[t], l[t][0]);
-    }
+    store_row<D>(a, out, parts, n.first_part + w.part, rows.start + my / a.group, w.kv_head * a.group + my % a.group, g, ref[t],
+                 l[t][0], sum[t]);
   }
 }
 
-// One wave adds up the parts of one (row, head): those of its own tokens that its sequence is long enough for, and all of the prefix.
-template <int D>
-__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, AttendPlan plan) {
-  const int lane = threadIdx.x & 63;
-  const int64_t task = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+// Adds up the parts of one (row, head): those of its own tokens that its sequence is long enough for, and all of the prefix.  WAVES of a workgroup of
+// four take one: parts go to its half waves in turn, 4 (D 64: 2) channels a lane, and a half wave's loads do not wait for each other.
+template <int D, int WAVES>
+__global__ __launch_bounds__(64 * kWaves) void attend_join_kernel(AttendArgs a, AttendPlan plan) {
+  constexpr int C = D / 32, kHalves = 2 * WAVES;
+  typedef float vec __attribute__((ext_vector_type(C)));
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t task = WAVES == 1 ? static_cast<int64_t>(blockIdx.x) * kWaves + wave : static_cast<int64_t>(blockIdx.x);
   const int row = static_cast<int>(task / a.q_heads), head = static_cast<int>(task % a.q_heads);
   if (row >= a.M) return;
   int seq = row;
@@ -656,23 +720,75 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, AttendPl
   const int last = (min((tile + 1) * tile_rows, count * a.group) - 1) / a.group;
   const int steps = steps_of(a, plan.own.over, plan.own.row_tiles ? kStage : kStep, own_tokens(a, seq), rows.count, last);
   const int filled = max(1, (steps + plan.own.steps - 1) / plan.own.steps);
-  const int apart = plan.prefix.grid ? plan.prefix.parts : 0;
+  const int total = filled + (plan.prefix.grid ? plan.prefix.parts : 0);
   const Part<D> in(a, plan.parts);
-  float ref = kNoScore, l = 0.f, y[D / 64] = {};
-  for (int k = 0; k < filled + apart; ++k) {
+  const int half = WAVES == 1 ? lane >> 5 : threadIdx.x >> 5, ch = (lane & 31) * C;
+  auto place = [&](int k) {
     const int p = k < filled ? plan.own.first_part + k : plan.prefix.first_part + k - filled;
-    const int64_t at = (static_cast<int64_t>(p) * a.M + row) * a.q_heads + head;
-    const float2 s = in.stats[at];
-    const float top = fmaxf(ref, s.x), mine = __builtin_amdgcn_exp2f(ref - top), theirs = __builtin_amdgcn_exp2f(s.x - top);
-    l = l * mine + s.y * theirs;
+    return (static_cast<int64_t>(p) * a.M + row) * a.q_heads + head;
+  };
+  float ref = kNoScore, l = 0.f;
+  vec y = {};
+  for (int k0 = half; k0 < total; k0 += 4 * kHalves) {
+    float2 s[4];
+    vec v[4];
 #pragma unroll
-    for (int e = 0; e < D / 64; ++e) y[e] = y[e] * mine + in.sums[at * D + lane * (D / 64) + e] * theirs;
+    for (int u = 0; u < 4; ++u) {
+      const int k = k0 + u * kHalves;
+      const int64_t at = place(min(k, total - 1));
+      s[u] = in.stats[at];
+      v[u] = *reinterpret_cast<const vec*>(in.sums + at * D + ch);
+      if (k >= total) s[u] = make_float2(kNoScore, 0.f);
+    }
+    float top = ref;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) top = fmaxf(top, s[u].x);
+    const float mine = __builtin_amdgcn_exp2f(ref - top);
+    l *= mine;
+    y *= mine;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (k0 + u * kHalves >= total) continue;
+      const float theirs = __builtin_amdgcn_exp2f(s[u].x - top);
+      l += s[u].y * theirs;
+      y += v[u] * theirs;
+    }
     ref = top;
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+  // the half waves' shares, in their order
+  __shared__ float lds_sum[WAVES == 1 ? 1 : kHalves][D], lds_ref[kHalves], lds_l[kHalves];
+  if constexpr (WAVES == 1) {
+    const float other = __shfl_xor(ref, 32, 64), top = fmaxf(ref, other), mine = __builtin_amdgcn_exp2f(ref - top);
+    l *= mine;
+    l += __shfl_xor(l, 32, 64);
 #pragma unroll
-  for (int e = 0; e < D / 64; ++e)
-    static_cast<_Float16*>(a.y)[row * a.ldy + head * D + lane * (D / 64) + e] = static_cast<_Float16>(y[e] * inv);
+    for (int e = 0; e < C; ++e) {
+      y[e] *= mine;
+      y[e] += __shfl_xor(y[e], 32, 64);
+    }
+  } else {
+    if ((lane & 31) == 0) { lds_ref[half] = ref; lds_l[half] = l; }
+#pragma unroll
+    for (int e = 0; e < C; ++e) lds_sum[half][ch + e] = y[e];
+    __syncthreads();
+    if (wave != 0) return;
+    float top = kNoScore;
+    for (int h = 0; h < kHalves; ++h) top = fmaxf(top, lds_ref[h]);
+    l = 0.f;
+    y = vec{};
+    for (int h = 0; h < kHalves; ++h) {
+      const float theirs = __builtin_amdgcn_exp2f(lds_ref[h] - top);
+      l += lds_l[h] * theirs;
+#pragma unroll
+      for (int e = 0; e < C; ++e) y[e] += lds_sum[h][ch + e] * theirs;
+    }
+  }
+  if (lane >= 32) return;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  _Float16* to = static_cast<_Float16*>(a.y) + row * a.ldy + head * D + ch;
+#pragma unroll
+  for (int e = 0; e < C; e += 2)
+    *reinterpret_cast<half2v*>(to + e) = half2v{static_cast<_Float16>(y[e] * inv), static_cast<_Float16>(y[e + 1] * inv)};
 }
 
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -689,8 +805,10 @@ static AttendLaunch shape_launch(const AttendArgs& a, int over, int64_t rows, in
   const int64_t parts = std::clamp<int64_t>((n.row_tiles ? 512 : 2048) / groups, 1, std::max<int64_t>(1, all / (n.row_tiles ? 2 : 8)));
   n.steps = static_cast<int>(ceil_div(all, parts));
   n.parts = static_cast<int>(ceil_div(all, n.steps));
-  n.by_xcd = pairs >= 8 && (pairs % 8 == 0 || pairs >= 64);
+  n.alone = n.row_tiles == 0 && groups * n.parts >= 2048 && n.steps <= 16;
+  n.by_xcd = !n.alone && pairs >= 8 && (pairs % 8 == 0 || pairs >= 64);
   n.grid = (n.by_xcd ? ceil_div(pairs, 8) * 8 : pairs) * n.tiles * n.parts;
+  if (n.alone) n.grid = ceil_div(n.grid, kWaves);
   return n;
 }
 
@@ -711,7 +829,8 @@ AttendPlan plan_attention(const AttendArgs& a) {
 
 template <int D, int BITS> static void launch_one(const AttendArgs& a, const AttendLaunch& n, int parts, hipStream_t st) {
   const dim3 grid(static_cast<unsigned>(n.grid)), block(64 * kWaves);
-  if (n.row_tiles == 0) attend_kernel<D, BITS><<<grid, block, 0, st>>>(a, n, parts);
+  if (n.row_tiles == 0 && n.alone) attend_kernel<D, BITS, 1><<<grid, block, 0, st>>>(a, n, parts);
+  else if (n.row_tiles == 0) attend_kernel<D, BITS, 4><<<grid, block, 0, st>>>(a, n, parts);
   else if (n.row_tiles == 1) attend_tile_kernel<D, BITS, 1><<<grid, block, 0, st>>>(a, n, parts);
   else attend_tile_kernel<D, BITS, 2><<<grid, block, 0, st>>>(a, n, parts);
 }
@@ -719,8 +838,9 @@ template <int D, int BITS> static void launch_one(const AttendArgs& a, const Att
 template <int D, int BITS> static int run(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
   if (p.prefix.grid) launch_one<D, BITS>(a, p.prefix, p.parts, st);
   launch_one<D, BITS>(a, p.own, p.parts, st);
-  if (p.parts > 1)
-    attend_join_kernel<D><<<static_cast<unsigned>(ceil_div(static_cast<int64_t>(a.M) * a.q_heads, 4)), 256, 0, st>>>(a, p);
+  const int64_t outputs = static_cast<int64_t>(a.M) * a.q_heads;
+  if (p.parts > 16) attend_join_kernel<D, 4><<<static_cast<unsigned>(outputs), 64 * kWaves, 0, st>>>(a, p);
+  else if (p.parts > 1) attend_join_kernel<D, 1><<<static_cast<unsigned>(ceil_div(outputs, kWaves)), 64 * kWaves, 0, st>>>(a, p);
   const hipError_t e = hipGetLastError();
   if (e == hipSuccess) return ROSAQ_OK;
   set_error(std::string("attention: ") + hipGetErrorString(e));
