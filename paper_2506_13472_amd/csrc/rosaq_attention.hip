@@ -47,19 +47,21 @@ __device__ __forceinline__ int steps_of(const AttendArgs& a, int over, int step,
 }
 
 // A workgroup's share of a launch.  Workgroups go to the XCDs in turn; with by_xcd, those of one sequence and kv head, which read
-// the same codes, stay on one XCD and its L2.  Tiles go from the last to the first, which under the causal mask is from the longest.
+// the same codes, stay on one XCD and its L2.  They are handed out from the last tile of all sequences to the first, which
+// under the causal mask is from the longest: what runs last is short.
 struct Share { int seq, kv_head, tile, part; bool any; };
 __device__ __forceinline__ Share share_of(const AttendArgs& a, const AttendLaunch& n, int id) {
-  const int heads = a.cache.kv_heads, seqs = n.over == kPrefix ? 1 : a.seqs, each = n.tiles * n.parts;
+  const int heads = a.cache.kv_heads, pairs = (n.over == kPrefix ? 1 : a.seqs) * heads;
   int pair, rest;
   if (n.by_xcd) {
-    pair = (id >> 3) / each * 8 + (id & 7);
-    rest = (id >> 3) % each;
+    const int each = (pairs + 7) / 8;
+    pair = (id >> 3) % each * 8 + (id & 7);
+    rest = (id >> 3) / each;
   } else {
-    pair = id / each;
-    rest = id % each;
+    pair = id % pairs;
+    rest = id / pairs;
   }
-  return Share{pair / heads, pair % heads, n.tiles - 1 - rest / n.parts, rest % n.parts, pair < seqs * heads};
+  return Share{pair / heads, pair % heads, n.tiles - 1 - rest / n.parts, rest % n.parts, pair < pairs && rest < n.tiles * n.parts};
 }
 
 // rows of a launch's sequence: with kPrefix all rows of the call are one
@@ -108,6 +110,42 @@ template <int BITS> __device__ __forceinline__ half2v value_pair(const uint32_t*
     const uint32_t d = w[2 * (j / 2) + t];
     return as_h2(__builtin_amdgcn_perm(0x64646464u, d, j % 2 == 0 ? 0x04020400u : 0x04030401u)) + c_lo;
   }
+}
+
+// The records of a step over one sequence's tokens or the prefix: N of them, from record block0 on.  look_up fetches the pages, a
+// step ahead of their use; place turns them into offsets and says which records have no page (those read the cache's first, and are hidden).
+// Where a page holds whole steps, one entry is enough, and records behind the last token are in the same page.
+template <int N> struct Pages { int page[N]; };
+template <int N> __device__ __forceinline__ Pages<N> look_up(const int32_t* table, int block0, int blocks, int block_shift) {
+  Pages<N> p;
+  if ((1 << block_shift) >= N) {
+    p.page[0] = block0 < blocks ? table[block0 >> block_shift] : -1;
+  } else {
+#pragma unroll
+    for (int b = 0; b < N; ++b) p.page[b] = block0 + b < blocks ? table[(block0 + b) >> block_shift] : -1;
+  }
+  return p;
+}
+template <int N>
+__device__ __forceinline__ int place(const CacheDev& c, const Pages<N>& p, int block0, int block_shift, int record, int64_t (&at)[N]) {
+  int hidden = 0;
+  if ((1 << block_shift) >= N) {
+    const int page = __builtin_amdgcn_readfirstlane(p.page[0]);
+    const bool bad = static_cast<unsigned>(page) >= static_cast<unsigned>(c.num_pages);
+    if (bad) hidden = (1 << N) - 1;
+    const int64_t first = (bad ? 0 : page) * c.page_bytes + (block0 & ((1 << block_shift) - 1)) * record;
+#pragma unroll
+    for (int b = 0; b < N; ++b) at[b] = first + b * record;
+  } else {
+#pragma unroll
+    for (int b = 0; b < N; ++b) {
+      const int page = __builtin_amdgcn_readfirstlane(p.page[b]);
+      const bool bad = static_cast<unsigned>(page) >= static_cast<unsigned>(c.num_pages);
+      if (bad) hidden |= 1 << b;
+      at[b] = (bad ? 0 : page) * c.page_bytes + ((block0 + b) & ((1 << block_shift) - 1)) * record;
+    }
+  }
+  return hidden;
 }
 
 __device__ __forceinline__ half2v minus(float bias, half2v z) {
@@ -210,21 +248,17 @@ __global__ __launch_bounds__(64 * kWaves, D == 128 && BITS == 8 ? 2 : 3) void at
   const char* head_base = c.base + kv_head * c.head_bytes;
   const int32_t* own_pages = a.pages + static_cast<int64_t>(seq) * a.page_stride;
 
-  auto load = [&](int step, Step<D, BITS>& x) {
+  auto pages_of = [&](int step) {
     const bool own = step >= prefix_steps;
-    const int block0 = (own ? step - prefix_steps : step) * 2;
-    const int32_t* table = own ? own_pages : a.prefix_pages;
-    const int blocks = ((own ? tokens : a.prefix_len) + kCacheBlock - 1) / kCacheBlock;
-    x.hidden = 0;
+    return look_up<2>(own ? own_pages : a.prefix_pages, (own ? step - prefix_steps : step) * 2,
+                      step < end ? ((own ? tokens : a.prefix_len) + kCacheBlock - 1) / kCacheBlock : 0, block_shift);
+  };
+  auto load = [&](int step, const Pages<2>& pages, Step<D, BITS>& x) {
+    int64_t at[2];
+    x.hidden = place<2>(c, pages, (step >= prefix_steps ? step - prefix_steps : step) * 2, block_shift, kRecord, at);
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      const int block = block0 + b;
-      int page = block < blocks ? table[block >> block_shift] : -1;
-      page = __builtin_amdgcn_readfirstlane(page);
-      const bool bad = page < 0 || page >= c.num_pages;
-      x.hidden |= bad ? 1 << b : 0;
-      // a record without a page is hidden below; the loads then take the cache's first one
-      const char* rec = head_base + (bad ? 0 : page * c.page_bytes + static_cast<int64_t>(block & ((1 << block_shift) - 1)) * kRecord);
+      const char* rec = head_base + at[b];
       load_codes(x.k[b], rec, r * 4 + g);
       load_codes(x.v[b], rec + kCodes, lane);
       const uint32_t* sz = reinterpret_cast<const uint32_t*>(rec + 2 * kCodes);
@@ -311,15 +345,23 @@ __global__ __launch_bounds__(64 * kWaves, D == 128 && BITS == 8 ? 2 : 3) void at
   constexpr int kTurn = SPLIT == 1 ? 1 : kWaves;
   int step = begin + (SPLIT == 1 ? 0 : wave);
   if (step < end) {
-    // two steps' codes: one is multiplied while the next is on its way
+    // two steps' codes: one is multiplied while the next is on its way, and the pages of the one after
     Step<D, BITS> x, y;
-    load(step, x);
+    Pages<2> next = pages_of(step);
+    load(step, next, x);
+    next = pages_of(step + kTurn);
     while (true) {
-      if (step + kTurn < end) load(step + kTurn, y);
+      if (step + kTurn < end) {
+        load(step + kTurn, next, y);
+        next = pages_of(step + 2 * kTurn);
+      }
       multiply(step, x);
       step += kTurn;
       if (step >= end) break;
-      if (step + kTurn < end) load(step + kTurn, x);
+      if (step + kTurn < end) {
+        load(step + kTurn, next, x);
+        next = pages_of(step + 2 * kTurn);
+      }
       multiply(step, y);
       step += kTurn;
       if (step >= end) break;
@@ -458,27 +500,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
   const uint32_t k_at = (r * 4 + g) * (Codes::kKey == 2 ? 8 : 16);
   const uint32_t v_at = kCodes + (kAllUnits == 4 ? (wave & 1) * 1024 + lane * 16 : (kAllUnits == 2 ? lane * 16 + (wave & 1) * 8 : lane * 8));
 
-  // pages of a stage's records (-1: none), a stage ahead of their use
-  auto look_up = [&](int stage, int (&page)[4]) {
+  auto pages_of = [&](int stage) {
     const bool own = stage >= prefix_stages;
-    const int block0 = (own ? stage - prefix_stages : stage) * 4;
-    const int32_t* table = own ? own_pages : a.prefix_pages;
-    const int blocks = ((own ? tokens : a.prefix_len) + kCacheBlock - 1) / kCacheBlock;
-#pragma unroll
-    for (int b = 0; b < 4; ++b) page[b] = stage < end && block0 + b < blocks ? table[(block0 + b) >> block_shift] : -1;
+    return look_up<4>(own ? own_pages : a.prefix_pages, (own ? stage - prefix_stages : stage) * 4,
+                      stage < end ? ((own ? tokens : a.prefix_len) + kCacheBlock - 1) / kCacheBlock : 0, block_shift);
   };
   // loads this wave's share of a stage
-  auto load = [&](int stage, const int (&pages)[4], Codes& x) {
-    const int block0 = (stage >= prefix_stages ? stage - prefix_stages : stage) * 4;
+  auto load = [&](int stage, const Pages<4>& pages, Codes& x) {
     int64_t at[4];
-    x.hidden = 0;
-#pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      const int page = __builtin_amdgcn_readfirstlane(pages[b]);
-      const bool bad = page < 0 || page >= c.num_pages;
-      x.hidden |= bad ? 1 << b : 0;
-      at[b] = bad ? 0 : page * c.page_bytes + static_cast<int64_t>((block0 + b) & ((1 << block_shift) - 1)) * kRecord;
-    }
+    x.hidden = place<4>(c, pages, (stage >= prefix_stages ? stage - prefix_stages : stage) * 4, block_shift, kRecord, at);
     const int64_t pair[2] = {wave < 2 ? at[0] : at[2], wave < 2 ? at[1] : at[3]};
     const char* mine = head_base + (wave & 1 ? pair[1] : pair[0]);
 #pragma unroll
@@ -514,26 +544,21 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
     const int held = (own ? tokens : a.prefix_len) - t0;
     const half2v own_sz = as_h2(x.k_own);
     const half2v z = {own_sz.y, own_sz.y}, k_lo = minus(1024.f, z), k_hi = minus(64.f, z);
-    // a value that is NaN reaches the rows that see it through their scores (the product has zero for it)
+    // a value that is NaN reaches the rows that see it through their scores
     if (g == 0) to.scale[wave * kCacheBlock + r] = (x.v_own & 0x7c00u) == 0x7c00u ? NAN : static_cast<float>(own_sz.x) * a.scale_log2;
 #pragma unroll
     for (int s = 0; s < KS; ++s)
       to.k[wave][s][lane] = __builtin_bit_cast(uint4, key_factor<BITS>(&x.k[s * BITS / 4], k_lo, k_hi));
     uint32_t sz[2][4];
-    uint32_t odd = 0;
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      sz[b][0] = x.v_sz[b].x; sz[b][1] = x.v_sz[b].y; sz[b][2] = x.v_sz[b].z; sz[b][3] = x.v_sz[b].w;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) odd = max(odd, sz[b][i] & 0x7c00u);
-    }
-    if (held < kStage || x.hidden || __any(odd == 0x7c00u)) {       // NaN, written or never written, would make NaN of 0
+    for (int b = 0; b < 2; ++b) { sz[b][0] = x.v_sz[b].x; sz[b][1] = x.v_sz[b].y; sz[b][2] = x.v_sz[b].z; sz[b][3] = x.v_sz[b].w; }
+    if (held < kStage || x.hidden) {       // what no one has written
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         const int record = (wave & 2) + b;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (record * kCacheBlock + 4 * g + i >= held || (x.hidden >> record & 1) || (sz[b][i] & 0x7c00u) == 0x7c00u) sz[b][i] = 0u;
+          if (record * kCacheBlock + 4 * g + i >= held || (x.hidden >> record & 1)) sz[b][i] = 0u;
       }
     }
     half2v s2[2][2], c_lo[2][2], c_hi[2][2];
@@ -541,7 +566,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        s2[b][t] = as_h2(__builtin_amdgcn_perm(sz[b][2 * t + 1], sz[b][2 * t], 0x05040100u));
+        // the larger of NaN and 0 is 0: a value that is NaN has 0 in the product, which otherwise made NaN of rows that do not see it
+        s2[b][t] = __builtin_elementwise_max(as_h2(__builtin_amdgcn_perm(sz[b][2 * t + 1], sz[b][2 * t], 0x05040100u)), half2v{});
         const half2v vz = as_h2(__builtin_amdgcn_perm(sz[b][2 * t + 1], sz[b][2 * t], 0x07060302u));
         c_lo[b][t] = minus(1024.f, vz);
         c_hi[b][t] = minus(64.f, vz);
@@ -582,7 +608,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
     const int t0 = (own ? stage - prefix_stages : stage) * kStage;
     if (own && t0 >= most_seen) return;
     const bool masked = hidden != 0 || t0 + kStage > (own ? least : a.prefix_len);
-    floatx4 score[4][RT];
+    floatx4 score[4][RT];                // products, then scores less the reference
+    float base[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) base[t] = ref[t] == kNoScore ? 0.f : ref[t];
 #pragma unroll
     for (int s = 0; s < KS; ++s)         // a product never waits for the sum of the one before
 #pragma unroll
@@ -597,7 +626,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
 #pragma unroll
       for (int t = 0; t < RT; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) score[b][t][i] *= scale[i];
+        for (int i = 0; i < 4; ++i) score[b][t][i] = __builtin_fmaf(score[b][t][i], scale[i], -base[t]);
     }
     if (masked) {
 #pragma unroll
@@ -619,19 +648,22 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
       most[t] = score[0][t][0];
 #pragma unroll
       for (int i = 1; i < 16; ++i) most[t] = fmaxf(most[t], score[i / 4][t][i % 4]);
-      over |= most[t] > ref[t] + kRoom;
+      over |= most[t] > (ref[t] == kNoScore ? kNoScore : kRoom);
     }
     if (__any(over)) {
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
         most[t] = fmaxf(most[t], __shfl_xor(most[t], 16, 64));
         most[t] = fmaxf(most[t], __shfl_xor(most[t], 32, 64));
-        const float next = fmaxf(ref[t], most[t] - kLead);
-        const float down = __builtin_amdgcn_exp2f(ref[t] - next);
+        const bool first = ref[t] == kNoScore;       // the reference goes to the first scores, up or down
+        if (first && !(most[t] > kNoScore)) continue;
+        const float up = first ? most[t] - kLead : fmaxf(0.f, most[t] - kLead), down = first ? 0.f : __builtin_amdgcn_exp2f(-up);
         l[t] *= floatx4{down, down, down, down};
 #pragma unroll
         for (int j = 0; j < U; ++j) sum[t][j] *= floatx4{down, down, down, down};
-        ref[t] = next;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) score[i / 4][t][i % 4] -= up;
+        ref[t] = base[t] + up;
       }
     }
 #pragma unroll
@@ -645,7 +677,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
           const floatx4& x = score[2 * p + i / 2][t];
           const int e = i % 2 * 2;
           pk[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(
-              __builtin_amdgcn_exp2f(x[e] - ref[t]), __builtin_amdgcn_exp2f(x[e + 1] - ref[t])));
+              __builtin_amdgcn_exp2f(x[e]), __builtin_amdgcn_exp2f(x[e + 1])));
         }
         prob[t] = as_h8(uint4{pk[0], pk[1], pk[2], pk[3]});
         l[t] = mfma16(ones, prob[t], l[t]);
@@ -661,17 +693,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
 
   if (begin < end) {
     Codes x;
-    int page[4], hidden;
-    look_up(begin, page);
-    load(begin, page, x);
-    look_up(begin + 1, page);
+    int hidden;
+    Pages<4> next = pages_of(begin);
+    load(begin, next, x);
+    next = pages_of(begin + 1);
     store(begin, x, lds[0]);
     hidden = x.hidden;
     lds_barrier();
     for (int stage = begin, cur = 0; stage < end; ++stage, cur ^= 1) {
       if (stage + 1 < end) {
-        load(stage + 1, page, x);
-        look_up(stage + 2, page);
+        load(stage + 1, next, x);
+        next = pages_of(stage + 2);
       }
       if (!idle) multiply(stage, hidden, lds[cur]);
       if (stage + 1 < end) store(stage + 1, x, lds[cur ^ 1]);
