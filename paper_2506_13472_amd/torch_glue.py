@@ -56,33 +56,41 @@ def linear_batch(layers, x: torch.Tensor, ys=None, ws: torch.Tensor | None = Non
 
 
 # ---- the attention between the q/k/v projections and the output projection -----------------------------------------
+#
+# A launch of a few rows runs 3 to 5 us and takes as long to issue, so the checks are kept to what costs little: those of one call
+# take about 1.5 us.
 
-def _matrix(name: str, x: torch.Tensor, width: int, rows: int | None = None) -> torch.Tensor:
-    if not x.is_cuda or x.dtype != torch.float16 or x.dim() != 2 or x.stride(1) != 1 or x.shape[1] != width:
-        raise ValueError(f"{name} must be a 2-D fp16 CUDA tensor of {width} columns with unit column stride")
-    if rows is not None and x.shape[0] != rows:
-        raise ValueError(f"{name} must have {rows} rows")
-    return x
+_HALF, _INT32, _INT64 = torch.float16, torch.int32, torch.int64
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
-def _integers(name: str, t: torch.Tensor, dtype: torch.dtype, count: int | None = None) -> int:
-    if not t.is_cuda or t.dtype != dtype or not t.is_contiguous() or (count is not None and t.numel() != count):
-        raise ValueError(f"{name} must be a contiguous {dtype} CUDA tensor" + (f" of {count} elements" if count is not None else ""))
+def _ld(name: str, x: torch.Tensor, rows: int, width: int) -> int:
+    """The row stride of an fp16 matrix [rows, width]; of a single row, whose stride torch leaves open, its width."""
+    if x.dtype is not _HALF or x.dim() != 2 or x.size(1) != width or x.size(0) != rows or x.stride(1) != 1:
+        raise ValueError(f"{name} must be an fp16 tensor [{rows}, {width}] with unit column stride")
+    return x.stride(0) if rows > 1 else width
+
+
+def _integers(name: str, t: torch.Tensor, dtype: torch.dtype, count: int) -> int:
+    """The address of a contiguous integer tensor of `count` elements (of any number: -1)."""
+    if t.dtype is not dtype or (t.numel() != count and count >= 0) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor" + (f" of {count} elements" if count >= 0 else ""))
     return t.data_ptr()
 
 
-def _on_device_of(*tensors) -> torch.cuda.device | None:
-    """A guard that makes the tensors' device current, or None where it is; raises where they lie on several."""
-    index = tensors[0].device.index
-    for t in tensors[1:]:
-        if t is not None and t.device.index != index:
-            raise ValueError("the tensors of a call must lie on one device")
-    return None if index == torch.cuda.current_device() else torch.cuda.device(index)
+def _device_of(*tensors) -> int:
+    """The GPU that all of a call's tensors (those that are not None) lie on."""
+    index = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != index:
+            raise ValueError("the tensors of a call must lie on one GPU")
+    if index < 0:
+        raise ValueError("the tensors of a call must lie on a GPU")
+    return index
 
 
-def _ld(x: torch.Tensor) -> int:
-    """Row stride; of a single row, whose stride torch leaves open, its width."""
-    return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+def _stream_on(index: int) -> int:
+    return _raw_stream(index) if _raw_stream is not None else torch.cuda.current_stream(index).cuda_stream
 
 
 class Rope:
@@ -110,16 +118,16 @@ def rope_table(positions: int, rot_dim: int, base: float = 10000.0, scaling: int
 def rope(r: Rope, x: torch.Tensor, positions: torch.Tensor, head_dim: int, out: torch.Tensor | None = None) -> torch.Tensor:
     """x with its heads turned to their rows' positions (int32 [M]); out may be x."""
     M, width = x.shape
-    _matrix("x", x, width)
+    ldx = _ld("x", x, M, width)
     if width % head_dim:
         raise ValueError("x must hold whole heads")
-    at = _integers("positions", positions, torch.int32, M)
-    guard = _on_device_of(x, positions, r.table, out)
-    if guard:
-        with guard:
+    at = _integers("positions", positions, _INT32, M)
+    device = _device_of(x, positions, r.table, out)
+    if device != _current_device():
+        with torch.cuda.device(device):
             return rope(r, x, positions, head_dim, out)
-    y = torch.empty_like(x, memory_format=torch.contiguous_format) if out is None else _matrix("out", out, width, M)
-    B.rosaq_rope(r.args, at, x.data_ptr(), M, _ld(x), width // head_dim, head_dim, y.data_ptr(), _ld(y), current_stream_ptr())
+    y = torch.empty((M, width), dtype=_HALF, device=x.device) if out is None else out
+    B.rosaq_rope(r.args, at, x.data_ptr(), M, ldx, width // head_dim, head_dim, y.data_ptr(), _ld("out", y, M, width), _stream_on(device))
     return y
 
 
@@ -137,49 +145,47 @@ def cache_append(cache: KvCache, slots: torch.Tensor, k: torch.Tensor, v: torch.
                  positions: torch.Tensor | None = None, q: torch.Tensor | None = None, q_out: torch.Tensor | None = None):
     """rosaq_cache_append: keys and values of M tokens to their slots (int64 [M]), keys turned first where `rope` is given, and
     the queries q beside them.  Returns the turned queries (None without q); q_out may be q."""
-    M = k.shape[0]
-    _matrix("k", k, cache.width)
-    _matrix("v", v, cache.width, M)
-    at_slots = _integers("slots", slots, torch.int64, M)
-    at = 0
-    if rope is not None:
+    M = k.size(0)
+    ldk, ldv = _ld("k", k, M, cache.width), _ld("v", v, M, cache.width)
+    at_slots = _integers("slots", slots, _INT64, M)
+    if rope is None:
+        if q is not None:
+            raise ValueError("q is only read to be turned: rope is missing")
+        device, angles, at = _device_of(k, v, slots, cache.data), None, 0
+    else:
         if positions is None:
             raise ValueError("rope needs positions")
-        at = _integers("positions", positions, torch.int32, M)
-    elif q is not None:
-        raise ValueError("q is only read to be turned: rope is missing")
-    guard = _on_device_of(k, v, slots, cache.data, positions, q, q_out, None if rope is None else rope.table)
-    if guard:
-        with guard:
+        at = _integers("positions", positions, _INT32, M)
+        device, angles = _device_of(k, v, slots, cache.data, positions, rope.table, q, q_out), rope.args
+    if device != _current_device():
+        with torch.cuda.device(device):
             return cache_append(cache, slots, k, v, rope, positions, q, q_out)
     if q is None:
-        B.rosaq_cache_append(cache.args, at_slots, M, k.data_ptr(), _ld(k), v.data_ptr(), _ld(v),
-                             None if rope is None else rope.args, at, stream=current_stream_ptr())
+        B.rosaq_cache_append(cache.args, at_slots, M, k.data_ptr(), ldk, v.data_ptr(), ldv, angles, at, stream=_stream_on(device))
         return None
-    _matrix("q", q, q.shape[1], M)
-    if q.shape[1] % cache.head_dim:
+    width = q.size(-1)
+    ldq = _ld("q", q, M, width)
+    if width % cache.head_dim:
         raise ValueError("q must hold whole heads")
-    y = torch.empty_like(q, memory_format=torch.contiguous_format) if q_out is None else _matrix("q_out", q_out, q.shape[1], M)
-    B.rosaq_cache_append(cache.args, at_slots, M, k.data_ptr(), _ld(k), v.data_ptr(), _ld(v), rope.args, at, q.data_ptr(), _ld(q),
-                         q.shape[1] // cache.head_dim, y.data_ptr(), _ld(y), current_stream_ptr())
+    y = torch.empty((M, width), dtype=_HALF, device=q.device) if q_out is None else q_out
+    B.rosaq_cache_append(cache.args, at_slots, M, k.data_ptr(), ldk, v.data_ptr(), ldv, angles, at, q.data_ptr(), ldq,
+                         width // cache.head_dim, y.data_ptr(), _ld("q_out", y, M, width), _stream_on(device))
     return y
 
 
 def cache_read(cache: KvCache, slots: torch.Tensor, k: torch.Tensor | None = None, v: torch.Tensor | None = None):
     """rosaq_cache_read: (k, v), the values of the slots; both are allocated where neither is given, one alone is read alone."""
     M = slots.numel()
-    at = _integers("slots", slots, torch.int64)
-    guard = _on_device_of(slots, cache.data, k, v)
-    if guard:
-        with guard:
+    at = _integers("slots", slots, _INT64, M)
+    device = _device_of(slots, cache.data, k, v)
+    if device != _current_device():
+        with torch.cuda.device(device):
             return cache_read(cache, slots, k, v)
     if k is None and v is None:
-        k, v = (torch.empty((M, cache.width), dtype=torch.float16, device=slots.device) for _ in range(2))
-    for name, x in (("k", k), ("v", v)):
-        if x is not None:
-            _matrix(name, x, cache.width, M)
-    B.rosaq_cache_read(cache.args, at, M, 0 if k is None else k.data_ptr(), 0 if k is None else _ld(k),
-                       0 if v is None else v.data_ptr(), 0 if v is None else _ld(v), current_stream_ptr())
+        k, v = (torch.empty((M, cache.width), dtype=_HALF, device=slots.device) for _ in range(2))
+    pk, ldk = (0, 0) if k is None else (k.data_ptr(), _ld("k", k, M, cache.width))
+    pv, ldv = (0, 0) if v is None else (v.data_ptr(), _ld("v", v, M, cache.width))
+    B.rosaq_cache_read(cache.args, at, M, pk, ldk, pv, ldv, _stream_on(device))
     return k, v
 
 
@@ -188,15 +194,16 @@ class AttentionPlan:
 
     def __init__(self, cache: KvCache, q_heads: int, sequences: int, max_kv: int, max_rows: int = 1, rows: int | None = None,
                  prefix_len: int = 0, causal: bool = True, scale: float | None = None):
-        """`rows`: rows of q, sequences * max_rows unless given."""
+        """`rows`: rows of q, sequences * max_rows unless given; scale: head_dim^-1/2 unless given."""
         self.cache = cache
+        self.M, self.width, self.sequences, self.prefix_len = sequences * max_rows if rows is None else rows, q_heads * cache.head_dim, sequences, prefix_len
         self.desc = B.AttentionDesc()
         d = self.desc
         d.cache = C.pointer(cache.args)
-        d.q_heads, d.sequences, d.max_kv, d.max_rows, d.prefix_len = q_heads, sequences, max_kv, max_rows, prefix_len
-        d.M = sequences * max_rows if rows is None else rows
+        d.q_heads, d.M, d.sequences, d.max_kv, d.max_rows, d.prefix_len = q_heads, self.M, sequences, max_kv, max_rows, prefix_len
         d.causal, d.scale = int(causal), cache.head_dim ** -0.5 if scale is None else scale
         self.ws = torch.empty(B.rosaq_workspace_bytes_attention(d), dtype=torch.uint8, device=cache.data.device)
+        self.ws_bytes = self.ws.numel()
 
 
 def attention(plan: AttentionPlan, q: torch.Tensor, kv_len: torch.Tensor, pages: torch.Tensor, row_start: torch.Tensor | None = None,
@@ -204,27 +211,27 @@ def attention(plan: AttentionPlan, q: torch.Tensor, kv_len: torch.Tensor, pages:
     """rosaq_attention: q [rows, q_heads * head_dim], kv_len int32 [sequences], pages int32 [sequences, pages of a sequence],
     row_start int32 [sequences + 1] (without it sequence b has row b), prefix_pages int32.  out must not overlap q; without it,
     rows that belong to no sequence are zero."""
-    d, cache = plan.desc, plan.cache
-    width = d.q_heads * cache.head_dim
-    _matrix("q", q, width, d.M)
-    at_len = _integers("kv_len", kv_len, torch.int32, d.sequences)
-    at_pages = _integers("pages", pages, torch.int32)
-    if pages.dim() != 2 or pages.shape[0] != d.sequences:
+    d, M = plan.desc, plan.M
+    ldq = _ld("q", q, M, plan.width)
+    if pages.dim() != 2 or pages.size(0) != plan.sequences:
         raise ValueError("pages must be [sequences, pages of a sequence]")
-    at_rows = None if row_start is None else _integers("row_start", row_start, torch.int32, d.sequences + 1)
+    at_len = _integers("kv_len", kv_len, _INT32, plan.sequences)
+    at_pages = _integers("pages", pages, _INT32, -1)
+    at_rows = None if row_start is None else _integers("row_start", row_start, _INT32, plan.sequences + 1)
     at_prefix = None
-    if d.prefix_len:
+    if plan.prefix_len:
         if prefix_pages is None:
             raise ValueError("the plan has a prefix: prefix_pages is missing")
-        at_prefix = _integers("prefix_pages", prefix_pages, torch.int32)
-        if prefix_pages.numel() * cache.page_tokens < d.prefix_len:
+        at_prefix = _integers("prefix_pages", prefix_pages, _INT32, -1)
+        if prefix_pages.numel() * plan.cache.page_tokens < plan.prefix_len:
             raise ValueError("prefix_pages hold fewer tokens than the prefix")
-    guard = _on_device_of(q, kv_len, pages, cache.data, row_start, prefix_pages, out)
-    if guard:
-        with guard:
+    device = _device_of(q, kv_len, pages, plan.ws, row_start, prefix_pages, out)
+    if device != _current_device():
+        with torch.cuda.device(device):
             return attention(plan, q, kv_len, pages, row_start, prefix_pages, out)
-    y = torch.zeros((d.M, width), dtype=torch.float16, device=q.device) if out is None else _matrix("out", out, width, d.M)
-    d.q, d.ldq, d.y, d.ldy = q.data_ptr(), _ld(q), y.data_ptr(), _ld(y)
-    d.kv_len, d.pages, d.page_stride, d.row_start, d.prefix_pages = at_len, at_pages, pages.shape[1], at_rows, at_prefix
-    B.rosaq_attention(d, plan.ws.data_ptr(), plan.ws.numel(), current_stream_ptr())
+    y = torch.zeros((M, plan.width), dtype=_HALF, device=q.device) if out is None else out
+    d.ldy = _ld("out", y, M, plan.width)
+    d.q, d.ldq, d.y = q.data_ptr(), ldq, y.data_ptr()
+    d.kv_len, d.pages, d.page_stride, d.row_start, d.prefix_pages = at_len, at_pages, pages.size(1), at_rows, at_prefix
+    B.rosaq_attention(d, plan.ws.data_ptr(), plan.ws_bytes, _stream_on(device))
     return y
