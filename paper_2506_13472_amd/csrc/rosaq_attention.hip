@@ -48,20 +48,15 @@ __device__ __forceinline__ int steps_of(const AttendArgs& a, int over, int step,
 
 // A workgroup's share of a launch.  Workgroups go to the XCDs in turn; with by_xcd, those of one sequence and kv head, which read
 // the same codes, stay on one XCD and its L2.  They are handed out from the last tile of all sequences to the first, which
-// under the causal mask is from the longest: what runs last is short.
+// under the causal mask is from the longest: what runs last is short.  The parts of a tile run side by side: the heads of a
+// sequence, on their XCDs, so read the same pages at a time (16 sequences of 8192 to 32768 tokens, 8 kv heads: 89 us, part by part 95).
 struct Share { int seq, kv_head, tile, part; bool any; };
 __device__ __forceinline__ Share share_of(const AttendArgs& a, const AttendLaunch& n, int id) {
   const int heads = a.cache.kv_heads, pairs = (n.over == kPrefix ? 1 : a.seqs) * heads;
-  int pair, rest;
-  if (n.by_xcd) {
-    const int each = (pairs + 7) / 8;
-    pair = (id >> 3) % each * 8 + (id & 7);
-    rest = (id >> 3) / each;
-  } else {
-    pair = id % pairs;
-    rest = id / pairs;
-  }
-  return Share{pair / heads, pair % heads, n.tiles - 1 - rest / n.parts, rest % n.parts, pair < pairs && rest < n.tiles * n.parts};
+  const int xcds = n.by_xcd ? 8 : 1, each = (pairs + xcds - 1) / xcds, turn = id / xcds;
+  const int part = turn % n.parts, rest = turn / n.parts;
+  const int pair = rest % each * xcds + id % xcds, tile = n.tiles - 1 - rest / each;
+  return Share{pair / heads, pair % heads, tile, part, pair < pairs && tile >= 0};
 }
 
 // rows of a launch's sequence: with kPrefix all rows of the call are one
