@@ -263,7 +263,7 @@ int rosaq_attention(const rosaq_attention_desc* desc, void* ws_dev, size_t ws_by
   const int rc = check_attention(desc, &a, true);
   if (rc != ROSAQ_OK) return rc;
   const AttendPlan p = plan_attention(a);
-  if (p.own.grid >= kMaxGrid || p.prefix.grid >= kMaxGrid) return fail(ROSAQ_ERR_SHAPE, "sequences x max_rows x q_heads too large: split the call");
+  if (p.own.grid + p.prefix.grid >= kMaxGrid) return fail(ROSAQ_ERR_SHAPE, "sequences x max_rows x q_heads too large: split the call");
   if (p.ws_bytes) {
     if (!ws_dev || ws_bytes < p.ws_bytes) return fail(ROSAQ_ERR_WORKSPACE, "workspace missing or too small");
     if (misaligned(ws_dev, 256)) return fail(ROSAQ_ERR_ALIGN, "workspace must be 256-byte aligned");

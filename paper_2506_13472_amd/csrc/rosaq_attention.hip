@@ -203,13 +203,17 @@ template <int D, int BITS> struct Step {
 // Values enter the product as the whole numbers code - z and their scale s in the other factor, P' = fp16(p s): one rounding for
 // a product of three numbers, and an operation less for each of the values, which with so few rows is where the time goes.  So
 // that P' is in fp16's range whatever the scales are, the reference is one of p s, not of p; the sum of p is fp32.
+template <int D> struct RowsLds {
+  float sum[kWaves][kRows][D + 4];
+  float ref[kWaves][kRows], l[kWaves][kRows];
+};
 template <int D, int BITS, int SPLIT>
-__global__ __launch_bounds__(64 * kWaves, D == 128 && BITS == 8 ? 2 : 3) void attend_kernel(AttendArgs a, AttendLaunch n, int parts) {
+__device__ __forceinline__ void attend_rows(const AttendArgs& a, const AttendLaunch& n, int parts, int block, RowsLds<D>& lds) {
   constexpr int U = D / 16, KS = D / 32;
   constexpr int kRecord = cache_record_bytes(D, BITS), kCodes = cache_code_bytes(D, BITS);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
-  const Share w = share_of(a, n, SPLIT == 1 ? static_cast<int>(blockIdx.x) * kWaves + wave : static_cast<int>(blockIdx.x));
+  const Share w = share_of(a, n, SPLIT == 1 ? block * kWaves + wave : block);
   if (!w.any) return;
   const int kv_head = w.kv_head, seq = w.seq, tile = w.tile;
   const Rows rows = rows_of(a, seq);
@@ -372,32 +376,30 @@ __global__ __launch_bounds__(64 * kWaves, D == 128 && BITS == 8 ? 2 : 3) void at
       store_row<D>(a, out, parts, part, rows.start + my_token, kv_head * a.group + my % a.group, g, ref, l, sum);
   } else {
     // the waves' shares, brought to one reference and added
-    __shared__ float lds_sum[kWaves][kRows][D + 4];
-    __shared__ float lds_ref[kWaves][kRows], lds_l[kWaves][kRows];
-    if (g == 0) { lds_ref[wave][r] = ref; lds_l[wave][r] = l; }
+    if (g == 0) { lds.ref[wave][r] = ref; lds.l[wave][r] = l; }
     __syncthreads();
-    float top = lds_ref[0][r];
+    float top = lds.ref[0][r];
 #pragma unroll
-    for (int o = 1; o < kWaves; ++o) top = fmaxf(top, lds_ref[o][r]);
+    for (int o = 1; o < kWaves; ++o) top = fmaxf(top, lds.ref[o][r]);
     const float down = __builtin_amdgcn_exp2f(ref - top);
     if (tile * kRows + r < used) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < U; ++j) lds_sum[wave][r][(4 * g + i) * U + j] = sum[j][i] * down;
+        for (int j = 0; j < U; ++j) lds.sum[wave][r][(4 * g + i) * U + j] = sum[j][i] * down;
     }
     __syncthreads();
     for (int e = threadIdx.x; e < kRows * D / 2; e += 64 * kWaves) {
       const int row = e / (D / 2), ch = e % (D / 2) * 2, at_row = tile * kRows + row;
       if (at_row >= used) break;
-      float t = lds_ref[0][row], total = 0.f, y0 = 0.f, y1 = 0.f;
+      float t = lds.ref[0][row], total = 0.f, y0 = 0.f, y1 = 0.f;
 #pragma unroll
-      for (int o = 1; o < kWaves; ++o) t = fmaxf(t, lds_ref[o][row]);
+      for (int o = 1; o < kWaves; ++o) t = fmaxf(t, lds.ref[o][row]);
 #pragma unroll
       for (int o = 0; o < kWaves; ++o) {
-        total += lds_l[o][row] * __builtin_amdgcn_exp2f(lds_ref[o][row] - t);
-        y0 += lds_sum[o][row][ch];
-        y1 += lds_sum[o][row][ch + 1];
+        total += lds.l[o][row] * __builtin_amdgcn_exp2f(lds.ref[o][row] - t);
+        y0 += lds.sum[o][row][ch];
+        y1 += lds.sum[o][row][ch + 1];
       }
       const int64_t token = rows.start + at_row / a.group;
       const int head = kv_head * a.group + at_row % a.group;
@@ -418,7 +420,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 128 && BITS == 8 ? 2 : 3) void at
 //
 // A workgroup of four waves takes 64 RT query rows of one sequence and kv head (of all rows of the call, over the prefix) and
 // stages of 64 tokens.  The codes become fp16 factors once a stage, a record's keys and half of two records' values a wave, and go to LDS as whole MFMA
-// operands (1 KiB, lane order), which all waves read; two stages' worth of LDS, so that one barrier a stage is enough.
+// operands (1 KiB, lane order), which all waves read.
 // Keys are multiplied as the whole numbers code - z and their scale acts on the scores, in fp32: rounded factors would be off by
 // 2^-11 of a score that may be in the hundreds.  Values are (code - z) s, rounded as reading the cache rounds them.  The sum of the
 // probabilities is one more MFMA, against ones.
@@ -432,6 +434,9 @@ template <int D, int BITS> struct StageCodes {
   uint4 v_sz[2];
   int hidden;                 // which of the stage's four records have no page
 };
+
+// Two stages' factors, so that one barrier a stage is enough; with one row tile a wave one stage's, which leaves room for three workgroups on a compute unit.
+constexpr int stage_buffers(int row_tiles) { return row_tiles == 1 ? 1 : 2; }
 
 template <int D> struct alignas(16) StageLds {
   uint4 k[4][D / 32][64];
@@ -447,14 +452,14 @@ __device__ __forceinline__ void lds_barrier() {
 }
 
 template <int D, int BITS, int RT>
-__global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs a, AttendLaunch n, int parts) {
+__device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLaunch& n, int parts, int block, StageLds<D> (&lds)[stage_buffers(RT)]) {
   constexpr int U = D / 16, KS = D / 32, kTileRows = 16 * RT * kWaves;
   constexpr int kRecord = cache_record_bytes(D, BITS), kCodes = cache_code_bytes(D, BITS);
+  constexpr int kBuffers = stage_buffers(RT);
   using Codes = StageCodes<D, BITS>;
-  __shared__ StageLds<D> lds[2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
-  const Share w = share_of(a, n, blockIdx.x);
+  const Share w = share_of(a, n, block);
   if (!w.any) return;
   const Rows rows = launch_rows(a, n.over, w.seq);
   const int used = (n.over == kPrefix ? rows.count : min(rows.count, a.max_rows)) * a.group;
@@ -700,8 +705,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
         load(stage + 1, next, x);
         next = pages_of(stage + 2);
       }
-      if (!idle) multiply(stage, hidden, lds[cur]);
-      if (stage + 1 < end) store(stage + 1, x, lds[cur ^ 1]);
+      if (!idle) multiply(stage, hidden, lds[kBuffers == 1 ? 0 : cur]);
+      if (kBuffers == 1) lds_barrier();
+      if (stage + 1 < end) store(stage + 1, x, lds[kBuffers == 1 ? 0 : cur ^ 1]);
       hidden = x.hidden;
       lds_barrier();
     }
@@ -715,6 +721,27 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
     store_row<D>(a, out, parts, n.first_part + w.part, rows.start + my / a.group, w.kv_head * a.group + my % a.group, g, ref[t],
                  l[t][0], sum[t]);
   }
+}
+
+template <int D, int BITS, int SPLIT>
+__global__ __launch_bounds__(64 * kWaves, D == 128 && BITS == 8 ? 2 : 3) void attend_rows_kernel(AttendArgs a, AttendLaunch n, int parts) {
+  __shared__ RowsLds<D> lds;
+  attend_rows<D, BITS, SPLIT>(a, n, parts, blockIdx.x, lds);
+}
+
+template <int D, int BITS, int RT>
+__global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs a, AttendLaunch n, int parts) {
+  __shared__ StageLds<D> lds[stage_buffers(RT)];
+  attend_tile<D, BITS, RT>(a, n, parts, blockIdx.x, lds);
+}
+
+// Both halves of a call whose prefix is apart, beside each other: the prefix for all rows, and behind those workgroups the sequences'
+// own tokens, of which there are too few to keep the card busy.
+template <int D, int BITS, int RT, int SPLIT>
+__global__ __launch_bounds__(64 * kWaves, RT == 1 && BITS == 4 ? 3 : 2) void attend_both_kernel(AttendArgs a, AttendLaunch prefix, AttendLaunch own, int parts) {
+  __shared__ union { StageLds<D> stages[stage_buffers(RT)]; RowsLds<D> rows; } lds;
+  if (blockIdx.x < prefix.grid) attend_tile<D, BITS, RT>(a, prefix, parts, blockIdx.x, lds.stages);
+  else attend_rows<D, BITS, SPLIT>(a, own, parts, blockIdx.x - static_cast<int>(prefix.grid), lds.rows);
 }
 
 // Adds up the parts of one (row, head): those of its own tokens that its sequence is long enough for, and all of the prefix.  WAVES of a workgroup of
@@ -829,7 +856,8 @@ static AttendLaunch shape_launch(const AttendArgs& a, int over, int64_t rows, in
   const int step = n.row_tiles ? kStage : kStep;
   const int64_t all = std::max<int64_t>(1, ceil_div(tokens_prefix, step) + ceil_div(tokens_own, step));
   const int64_t pairs = seqs * a.cache.kv_heads, groups = pairs * n.tiles;
-  const int64_t parts = std::clamp<int64_t>((n.row_tiles ? 512 : 2048) / groups, 1, std::max<int64_t>(1, all / (n.row_tiles ? 2 : 8)));
+  const int64_t fill = n.row_tiles == 0 ? 2048 : (n.row_tiles == 1 && over == kPrefix ? 256 : 512);
+  const int64_t parts = std::clamp<int64_t>(fill / groups, 1, std::max<int64_t>(1, all / (n.row_tiles ? 2 : 8)));
   n.steps = static_cast<int>(ceil_div(all, parts));
   n.parts = static_cast<int>(ceil_div(all, n.steps));
   n.alone = n.row_tiles == 0 && groups * n.parts >= 2048 && n.steps <= 16;
@@ -854,17 +882,28 @@ AttendPlan plan_attention(const AttendArgs& a) {
   return p;
 }
 
+template <int D, int BITS, int RT> static void launch_both(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
+  const dim3 grid(static_cast<unsigned>(p.prefix.grid + p.own.grid)), block(64 * kWaves);
+  if (p.own.alone) attend_both_kernel<D, BITS, RT, 1><<<grid, block, 0, st>>>(a, p.prefix, p.own, p.parts);
+  else attend_both_kernel<D, BITS, RT, 4><<<grid, block, 0, st>>>(a, p.prefix, p.own, p.parts);
+}
+
 template <int D, int BITS> static void launch_one(const AttendArgs& a, const AttendLaunch& n, int parts, hipStream_t st) {
   const dim3 grid(static_cast<unsigned>(n.grid)), block(64 * kWaves);
-  if (n.row_tiles == 0 && n.alone) attend_kernel<D, BITS, 1><<<grid, block, 0, st>>>(a, n, parts);
-  else if (n.row_tiles == 0) attend_kernel<D, BITS, 4><<<grid, block, 0, st>>>(a, n, parts);
+  if (n.row_tiles == 0 && n.alone) attend_rows_kernel<D, BITS, 1><<<grid, block, 0, st>>>(a, n, parts);
+  else if (n.row_tiles == 0) attend_rows_kernel<D, BITS, 4><<<grid, block, 0, st>>>(a, n, parts);
   else if (n.row_tiles == 1) attend_tile_kernel<D, BITS, 1><<<grid, block, 0, st>>>(a, n, parts);
   else attend_tile_kernel<D, BITS, 2><<<grid, block, 0, st>>>(a, n, parts);
 }
 
 template <int D, int BITS> static int run(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
-  if (p.prefix.grid) launch_one<D, BITS>(a, p.prefix, p.parts, st);
-  launch_one<D, BITS>(a, p.own, p.parts, st);
+  if (p.prefix.grid && p.own.row_tiles == 0) {
+    if (p.prefix.row_tiles == 1) launch_both<D, BITS, 1>(a, p, st);
+    else launch_both<D, BITS, 2>(a, p, st);
+  } else {
+    if (p.prefix.grid) launch_one<D, BITS>(a, p.prefix, p.parts, st);
+    launch_one<D, BITS>(a, p.own, p.parts, st);
+  }
   const int64_t outputs = static_cast<int64_t>(a.M) * a.q_heads;
   if (p.parts > 16) attend_join_kernel<D, 4><<<static_cast<unsigned>(outputs), 64 * kWaves, 0, st>>>(a, p);
   else if (p.parts > 1) attend_join_kernel<D, 1><<<static_cast<unsigned>(ceil_div(outputs, kWaves)), 64 * kWaves, 0, st>>>(a, p);
