@@ -361,7 +361,7 @@ typedef struct {
   int32_t max_kv;                   /* cached tokens of a sequence, without the prefix: at most this many (cut beyond) */
   int32_t prefix_len;               /* tokens of the shared prefix, 0 for none                          */
   int32_t causal;                   /* 0 or 1                                                           */
-  float scale;                      /* e.g. head_dim^-1/2                                               */
+  float scale;                      /* e.g. head_dim^-1/2; any sign, at most 2^60                       */
   const void* q_dev; int64_t ldq;   /* DEVICE fp16 [M x q_heads * head_dim], turned already             */
   void* y_dev; int64_t ldy;         /* DEVICE fp16 [M x q_heads * head_dim], apart from q; rows of no sequence stay as they are */
   const int32_t* row_start_dev;     /* DEVICE int32 [sequences + 1], ascending: sequence b has rows row_start[b] .. row_start[b+1] - 1. */

@@ -130,7 +130,7 @@ static int check_attention(const rosaq_attention_desc* d, AttendArgs* a, bool po
   if (d->max_rows < 1 || d->max_rows > d->M) return fail(ROSAQ_ERR_SHAPE, "max_rows must be in [1, M]");
   if (d->max_kv < 0 || d->prefix_len < 0) return fail(ROSAQ_ERR_SHAPE, "max_kv and prefix_len must not be negative");
   if (d->max_kv > (1 << 30) || d->prefix_len > (1 << 30)) return fail(ROSAQ_ERR_SHAPE, "max_kv and prefix_len go up to 2^30");
-  if (!std::isfinite(d->scale)) return fail(ROSAQ_ERR_ARG, "scale must be finite");
+  if (!(std::fabs(d->scale) <= 0x1p60f)) return fail(ROSAQ_ERR_ARG, "scale must be a number of at most 2^60");
   if (d->causal != 0 && d->causal != 1) return fail(ROSAQ_ERR_ARG, "causal must be 0 or 1");
   if (!pointers || !d->row_start_dev) {
     // without row starts every sequence has one row
@@ -157,7 +157,9 @@ static int check_attention(const rosaq_attention_desc* d, AttendArgs* a, bool po
   // a plan for max_kv tokens serves a table cut to the pages that are in use
   const int64_t room = pointers ? static_cast<int64_t>(d->page_stride) * shape.page_tokens : d->max_kv;
   a->max_rows = d->max_rows; a->max_kv = d->max_kv; a->capacity = static_cast<int>(room < d->max_kv ? room : d->max_kv); a->causal = d->causal;
-  a->scale_log2 = static_cast<float>(static_cast<double>(d->scale) * 1.4426950408889634);
+  // The kernels divide by the keys' scales times this.  Below 2^-60 it makes every score 0 to the last bit that counts (|q.k| < 2^40).
+  const double scale = static_cast<double>(d->scale) * 1.4426950408889634;
+  a->scale_log2 = static_cast<float>(std::fabs(scale) < 0x1p-60 ? 0x1p-60 : scale);
   a->dim = shape.head_dim; a->bits = shape.bits;
   a->part = nullptr;
   return ROSAQ_OK;

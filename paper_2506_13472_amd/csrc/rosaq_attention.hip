@@ -421,9 +421,11 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const AttendLau
 // A workgroup of four waves takes 64 RT query rows of one sequence and kv head (of all rows of the call, over the prefix) and
 // stages of 64 tokens.  The codes become fp16 factors once a stage, a record's keys and half of two records' values a wave, and go to LDS as whole MFMA
 // operands (1 KiB, lane order), which all waves read.
-// Keys are multiplied as the whole numbers code - z and their scale acts on the scores, in fp32: rounded factors would be off by
-// 2^-11 of a score that may be in the hundreds.  Values are (code - z) s, rounded as reading the cache rounds them.  The sum of the
-// probabilities is one more MFMA, against ones.
+// Both are the whole numbers code - z.  The keys' scale acts on the scores, in fp32: rounded factors would be off by 2^-11 of a
+// score that may be in the hundreds.  The values' scale is in the other factor, as in attend_rows, here through the exponent: P' = 2^(score + log2 s - reference),
+// with log2 s over the keys' scale as what the sum of a score starts from.
+// The sum of the probabilities is one more MFMA, of P' against fp16(1 / s): what the rounding of 1 / s does to it is the mean over the
+// tokens of 2^-12 either way.
 constexpr int kStage = 4 * kCacheBlock;
 
 template <int D, int BITS> struct StageCodes {
@@ -441,7 +443,9 @@ constexpr int stage_buffers(int row_tiles) { return row_tiles == 1 ? 1 : 2; }
 template <int D> struct alignas(16) StageLds {
   uint4 k[4][D / 32][64];
   uint4 v[2][D / 16][64];
-  float scale[kStage];        // of the keys, times scale_log2; NaN where a value is NaN
+  float scale[kStage];        // of the keys, times scale_log2
+  float start[kStage];        // log2 of the values' scales, over `scale`; NaN where a value is NaN
+  _Float16 inverse[kStage];   // of the values' scales; 0 where there is none
 };
 
 // Workgroup barrier that orders LDS traffic only: the next stage's codes stay in flight across it.
@@ -544,8 +548,15 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
     const int held = (own ? tokens : a.prefix_len) - t0;
     const half2v own_sz = as_h2(x.k_own);
     const half2v z = {own_sz.y, own_sz.y}, k_lo = minus(1024.f, z), k_hi = minus(64.f, z);
-    // a value that is NaN reaches the rows that see it through their scores
-    if (g == 0) to.scale[wave * kCacheBlock + r] = (x.v_own & 0x7c00u) == 0x7c00u ? NAN : static_cast<float>(own_sz.x) * a.scale_log2;
+    if (g == 0) {
+      // a value that is NaN reaches the rows that see it through their scores, and no other row
+      const int at = wave * kCacheBlock + r;
+      const float s = static_cast<float>(as_h2(x.v_own).x);
+      const float ks = static_cast<float>(own_sz.x) * a.scale_log2;
+      to.scale[at] = ks;
+      to.start[at] = __builtin_amdgcn_logf(s) * __builtin_amdgcn_rcpf(ks);
+      to.inverse[at] = at < held && s > 0.f && s < INFINITY ? static_cast<_Float16>(__builtin_amdgcn_rcpf(s)) : (_Float16)0.f;
+    }
 #pragma unroll
     for (int s = 0; s < KS; ++s)
       to.k[wave][s][lane] = __builtin_bit_cast(uint4, key_factor<BITS>(&x.k[s * BITS / 4], k_lo, k_hi));
@@ -561,13 +572,11 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
           if (record * kCacheBlock + 4 * g + i >= held || (x.hidden >> record & 1)) sz[b][i] = 0u;
       }
     }
-    half2v s2[2][2], c_lo[2][2], c_hi[2][2];
+    half2v c_lo[2][2], c_hi[2][2];
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        // the larger of NaN and 0 is 0: a value that is NaN has 0 in the product, which otherwise made NaN of rows that do not see it
-        s2[b][t] = __builtin_elementwise_max(as_h2(__builtin_amdgcn_perm(sz[b][2 * t + 1], sz[b][2 * t], 0x05040100u)), half2v{});
         const half2v vz = as_h2(__builtin_amdgcn_perm(sz[b][2 * t + 1], sz[b][2 * t], 0x07060302u));
         c_lo[b][t] = minus(1024.f, vz);
         c_hi[b][t] = minus(64.f, vz);
@@ -581,9 +590,9 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
         for (int t = 0; t < 2; ++t) {
           if constexpr (D == 64 && BITS == 4) {      // one unit holds all four channels
             const uint32_t mine[2] = {x.v[b][0] >> ((wave & 1) * 8), x.v[b][1] >> ((wave & 1) * 8)};
-            v[2 * b + t] = value_pair<BITS>(mine, j, t, c_lo[b][t], c_hi[b][t]) * s2[b][t];
+            v[2 * b + t] = value_pair<BITS>(mine, j, t, c_lo[b][t], c_hi[b][t]);
           } else {
-            v[2 * b + t] = value_pair<BITS>(x.v[b], j, t, c_lo[b][t], c_hi[b][t]) * s2[b][t];
+            v[2 * b + t] = value_pair<BITS>(x.v[b], j, t, c_lo[b][t], c_hi[b][t]);
           }
         }
       const half8 f = {v[0].x, v[0].y, v[1].x, v[1].y, v[2].x, v[2].y, v[3].x, v[3].y};
@@ -600,8 +609,6 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
 #pragma unroll
     for (int j = 0; j < U; ++j) sum[t][j] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
-  const _Float16 one = (_Float16)1.f;
-  const half8 ones = {one, one, one, one, one, one, one, one};
 
   auto multiply = [&](int stage, int hidden, const StageLds<D>& from) {
     const bool own = stage >= prefix_stages;
@@ -612,13 +619,16 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
     float base[RT];
 #pragma unroll
     for (int t = 0; t < RT; ++t) base[t] = ref[t] == kNoScore ? 0.f : ref[t];
+    floatx4 start[4];
+#pragma unroll
+    for (int b = 0; b < 4; ++b) start[b] = *reinterpret_cast<const floatx4*>(&from.start[b * kCacheBlock + 4 * g]);
 #pragma unroll
     for (int s = 0; s < KS; ++s)         // a product never waits for the sum of the one before
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
         const half8 f = as_h8(from.k[b][s][lane]);
 #pragma unroll
-        for (int t = 0; t < RT; ++t) score[b][t] = mfma16(f, q[t][s], s ? score[b][t] : floatx4{0.f, 0.f, 0.f, 0.f});
+        for (int t = 0; t < RT; ++t) score[b][t] = mfma16(f, q[t][s], s ? score[b][t] : start[b]);
       }
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
@@ -669,6 +679,9 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
       half8 prob[RT];
+      const uint2 inv0 = *reinterpret_cast<const uint2*>(&from.inverse[2 * p * kCacheBlock + 4 * g]);
+      const uint2 inv1 = *reinterpret_cast<const uint2*>(&from.inverse[(2 * p + 1) * kCacheBlock + 4 * g]);
+      const half8 inverse = as_h8(uint4{inv0.x, inv0.y, inv1.x, inv1.y});
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
         uint32_t pk[4];
@@ -676,11 +689,11 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
         for (int i = 0; i < 4; ++i) {
           const floatx4& x = score[2 * p + i / 2][t];
           const int e = i % 2 * 2;
-          pk[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(
-              __builtin_amdgcn_exp2f(x[e]), __builtin_amdgcn_exp2f(x[e + 1])));
+          pk[i] = __builtin_bit_cast(uint32_t, half2v{static_cast<_Float16>(__builtin_amdgcn_exp2f(x[e])),
+                                                      static_cast<_Float16>(__builtin_amdgcn_exp2f(x[e + 1]))});
         }
         prob[t] = as_h8(uint4{pk[0], pk[1], pk[2], pk[3]});
-        l[t] = mfma16(ones, prob[t], l[t]);
+        l[t] = mfma16(inverse, prob[t], l[t]);
       }
 #pragma unroll
       for (int j = 0; j < U; ++j) {

@@ -133,7 +133,7 @@ def test_attention_refusals():
     assert _code(lambda: f(max_rows=5, row_start=Z)) == SHAPE                                   # more than M
     assert _code(lambda: f(max_kv=-1)) == SHAPE and _code(lambda: f(prefix_len=-1)) == SHAPE
     assert _code(lambda: f(max_kv=(1 << 30) + 1, page_stride=1 << 30)) == SHAPE and _code(lambda: f(page_stride=-1)) == SHAPE
-    for s in (float("nan"), float("inf")):
+    for s in (float("nan"), float("inf"), -float("inf"), 2e18):
         assert _code(lambda: f(scale=s)) == ARG
     assert _code(lambda: f(causal=2)) == ARG
     assert _code(lambda: f(ldq=1000)) == SHAPE and _code(lambda: f(ldy=1028)) == ALIGN and _code(lambda: f(q=X + 2)) == ALIGN

@@ -366,6 +366,29 @@ def test_scores_that_grow_and_fall():
             b.check(b.run())
 
 
+@pytest.mark.parametrize("rows", [1, 20, 140])
+@pytest.mark.parametrize("scale", [0.0, -0.2, 1e-30, 3.0])
+def test_scales(rows, scale):
+    """A mean, the smallest scores first, and scores of some tens."""
+    print(f"case scale {scale} rows {rows}", flush=True)
+    b = Batch(19, [300], [rows], 2, 1, 64, 4, 32)
+    b.scale = scale
+    b.append()
+    b.check(b.run(b.plan(scale=scale)))
+
+
+@pytest.mark.parametrize("rows", [1, 20, 140])
+def test_values_and_keys_of_very_different_size(rows):
+    """Groups from subnormal to the largest numbers side by side: the scale of each acts on its own token only."""
+    print(f"case sizes rows {rows}", flush=True)
+    b = Batch(20, [400], [rows], 1, 2, 128, 8, 64)
+    size = 2.0 ** np.linspace(-24, 15, 400)[np.random.default_rng(0).permutation(400)]
+    b.v = (np.clip(b.v, -2, 2) * size[:, None]).astype(np.float16)
+    b.k = (np.clip(b.k, -2, 2) * np.minimum(size, 8.0)[::-1, None]).astype(np.float16)
+    b.append()
+    b.check(b.run())
+
+
 def test_one_token_outweighs_a_long_tail():
     """60000 tokens of which each weighs 2^-24 of the first: together they count."""
     print("case tail", flush=True)
