@@ -424,8 +424,8 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const AttendLau
 // Both are the whole numbers code - z.  The keys' scale acts on the scores, in fp32: rounded factors would be off by 2^-11 of a
 // score that may be in the hundreds.  The values' scale is in the other factor, as in attend_rows, here through the exponent: P' = 2^(score + log2 s - reference),
 // with log2 s over the keys' scale as what the sum of a score starts from.
-// The sum of the probabilities is one more MFMA, of P' against fp16(1 / s): what the rounding of 1 / s does to it is the mean over the
-// tokens of 2^-12 either way.
+// The sum of the probabilities, P' / s in fp32, takes P' before it is rounded: next to a token of large values, those of others may round to nothing,
+// which the product does not notice, but their weights would be missing here.
 constexpr int kStage = 4 * kCacheBlock;
 
 template <int D, int BITS> struct StageCodes {
@@ -445,7 +445,7 @@ template <int D> struct alignas(16) StageLds {
   uint4 v[2][D / 16][64];
   float scale[kStage];        // of the keys, times scale_log2
   float start[kStage];        // log2 of the values' scales, over `scale`; NaN where a value is NaN
-  _Float16 inverse[kStage];   // of the values' scales; 0 where there is none
+  float inverse[kStage];      // of the values' scales, 0 where that is no number
 };
 
 // Workgroup barrier that orders LDS traffic only: the next stage's codes stay in flight across it.
@@ -555,7 +555,8 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
       const float ks = static_cast<float>(own_sz.x) * a.scale_log2;
       to.scale[at] = ks;
       to.start[at] = __builtin_amdgcn_logf(s) * __builtin_amdgcn_rcpf(ks);
-      to.inverse[at] = at < held && s > 0.f && s < INFINITY ? static_cast<_Float16>(__builtin_amdgcn_rcpf(s)) : (_Float16)0.f;
+      // what a row does not see weighs 0 there, and 0 x NaN is NaN
+      to.inverse[at] = s > 0.f && s < INFINITY ? __builtin_amdgcn_rcpf(s) : 0.f;
     }
 #pragma unroll
     for (int s = 0; s < KS; ++s)
@@ -600,11 +601,11 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
     }
   };
 
-  floatx4 sum[RT][U], l[RT];
-  float ref[RT];
+  floatx4 sum[RT][U];
+  float ref[RT], l[RT];
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
-    l[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+    l[t] = 0.f;
     ref[t] = kNoScore;
 #pragma unroll
     for (int j = 0; j < U; ++j) sum[t][j] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -668,7 +669,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
         const bool first = ref[t] == kNoScore;       // the reference goes to the first scores, up or down
         if (first && !(most[t] > kNoScore)) continue;
         const float up = first ? most[t] - kLead : fmaxf(0.f, most[t] - kLead), down = first ? 0.f : __builtin_amdgcn_exp2f(-up);
-        l[t] *= floatx4{down, down, down, down};
+        l[t] *= down;
 #pragma unroll
         for (int j = 0; j < U; ++j) sum[t][j] *= floatx4{down, down, down, down};
 #pragma unroll
@@ -679,22 +680,17 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
       half8 prob[RT];
-      const uint2 inv0 = *reinterpret_cast<const uint2*>(&from.inverse[2 * p * kCacheBlock + 4 * g]);
-      const uint2 inv1 = *reinterpret_cast<const uint2*>(&from.inverse[(2 * p + 1) * kCacheBlock + 4 * g]);
-      const half8 inverse = as_h8(uint4{inv0.x, inv0.y, inv1.x, inv1.y});
+      floatx4 inverse[2];
 #pragma unroll
-      for (int t = 0; t < RT; ++t) {
-        uint32_t pk[4];
+      for (int b = 0; b < 2; ++b) inverse[b] = *reinterpret_cast<const floatx4*>(&from.inverse[(2 * p + b) * kCacheBlock + 4 * g]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const floatx4& x = score[2 * p + i / 2][t];
-          const int e = i % 2 * 2;
-          pk[i] = __builtin_bit_cast(uint32_t, half2v{static_cast<_Float16>(__builtin_amdgcn_exp2f(x[e])),
-                                                      static_cast<_Float16>(__builtin_amdgcn_exp2f(x[e + 1]))});
+      for (int t = 0; t < RT; ++t)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float e = __builtin_amdgcn_exp2f(score[2 * p + i / 4][t][i % 4]);
+          l[t] = __builtin_fmaf(e, inverse[i / 4][i % 4], l[t]);
+          prob[t][i] = static_cast<_Float16>(e);
         }
-        prob[t] = as_h8(uint4{pk[0], pk[1], pk[2], pk[3]});
-        l[t] = mfma16(inverse, prob[t], l[t]);
-      }
 #pragma unroll
       for (int j = 0; j < U; ++j) {
         const half8 f = as_h8(p == 0 ? ahead[j] : from.v[1][j][lane]);
@@ -730,9 +726,11 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
     const int my = first_row + 16 * t + r;
+    l[t] += __shfl_xor(l[t], 16, 64);
+    l[t] += __shfl_xor(l[t], 32, 64);
     if (my >= used) continue;
     store_row<D>(a, out, parts, n.first_part + w.part, rows.start + my / a.group, w.kv_head * a.group + my % a.group, g, ref[t],
-                 l[t][0], sum[t]);
+                 l[t], sum[t]);
   }
 }
 
