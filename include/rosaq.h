@@ -264,7 +264,7 @@ int rosaq_pca_full(const void* X_dev, int32_t n_cal, int32_t D, int64_t ldx, flo
  * cache as 4- or 8-bit codes, rosaq_attention reads the cache.  Matrices are as there: fp16 [M x heads * head_dim], a row's
  * heads side by side, row m at p + m * ld, 16-byte aligned, ld a multiple of 8.  All calls are asynchronous on hip_stream,
  * allocate nothing, never synchronise and may be captured into a graph; the current device must be the one that holds
- * the memory.  Outputs must not overlap inputs except where said.
+ * the memory.  Outputs must not overlap inputs except where said.  M times the heads of a call is at most 2^27.
  *
  * Integers in DEVICE memory are not seen by the host, so what they may hold is defined for every value: a slot, position or
  * page outside its range means "none" (see each call), lengths are cut to the capacity.  Nothing is read or written through them. */

@@ -17,7 +17,7 @@ static int fail(int code, const char* msg) {
 // Launches number 16 tasks a workgroup of 256 threads, and a grid has fewer than 2^32 threads.
 constexpr int64_t kMaxTasks = int64_t{1} << 27;
 constexpr int64_t kMaxGrid = int64_t{1} << 24;
-constexpr int kMaxRows = 1 << 20;      // as for the linear layers
+constexpr int kMaxSequences = 1 << 20;
 
 static bool misaligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n != 0; }
 
@@ -82,8 +82,7 @@ static int check_matrix(const char* name, const void* p, int64_t ld, int64_t wid
 
 static int check_rows(int32_t M, int64_t heads) {
   if (M < 1) return fail(ROSAQ_ERR_SHAPE, "M must be at least 1");
-  if (M > kMaxRows) return fail(ROSAQ_ERR_SHAPE, "M above 2^20: split the call");
-  if (M * heads > kMaxTasks) return fail(ROSAQ_ERR_SHAPE, "M x heads above 2^27: split the call");
+  if (static_cast<int64_t>(M) * heads > kMaxTasks) return fail(ROSAQ_ERR_SHAPE, "M x heads above 2^27: split the call");
   return ROSAQ_OK;
 }
 
@@ -126,7 +125,7 @@ static int check_attention(const rosaq_attention_desc* d, AttendArgs* a, bool po
   if (d->q_heads % shape.kv_heads) return fail(ROSAQ_ERR_SHAPE, "q_heads must be a multiple of the cache's kv_heads");
   rc = check_rows(d->M, d->q_heads);
   if (rc != ROSAQ_OK) return rc;
-  if (d->sequences < 1 || d->sequences > kMaxRows) return fail(ROSAQ_ERR_SHAPE, "sequences must be in [1, 2^20]");
+  if (d->sequences < 1 || d->sequences > kMaxSequences) return fail(ROSAQ_ERR_SHAPE, "sequences must be in [1, 2^20]");
   if (d->max_rows < 1 || d->max_rows > d->M) return fail(ROSAQ_ERR_SHAPE, "max_rows must be in [1, M]");
   if (d->max_kv < 0 || d->prefix_len < 0) return fail(ROSAQ_ERR_SHAPE, "max_kv and prefix_len must not be negative");
   if (d->max_kv > (1 << 30) || d->prefix_len > (1 << 30)) return fail(ROSAQ_ERR_SHAPE, "max_kv and prefix_len go up to 2^30");

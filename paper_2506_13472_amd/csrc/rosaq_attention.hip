@@ -878,10 +878,22 @@ static AttendLaunch shape_launch(const AttendArgs& a, int over, int64_t rows, in
   return n;
 }
 
+// Whether the prefix is computed for all sequences at once, apart from their own tokens: where it saves enough steps of rereading it
+// to pay for the partial results and the launch that joins them.  us, with every sequence / apart, own tokens up to 256:
+//   64 sequences x 32 heads, 4 bits: prefix of 64 tokens 19.9 / 21.0, 128 22.8 / 22.1, 512 40.2 / 24.6
+//   16 x 8 kv heads x 4, 8 bits: 512 tokens 12.5 / 12.6, 1024 15.5 / 13.5, 2048 21.3 / 14.2
+//   4 x 32, 4 bits: 512 11.5 / 11.4, 2048 17.9 / 16.3;  2 x 8 x 4: 4096 12.0 / 12.4;  32 x 4 rows x 8 x 4: 512 18.3 / 20.1
+// Rows that need more than one tile fill the matrix cores without their neighbours (16 x 12 rows x 8 x 4, 1024: 25.5 / 37.6).
+static bool prefix_apart(const AttendArgs& a) {
+  if (a.prefix_len == 0 || a.max_rows * static_cast<int64_t>(a.group) > kRows) return false;
+  const int64_t saved = static_cast<int64_t>(a.seqs - 1) * a.cache.kv_heads * ceil_div(a.prefix_len, kStep);
+  return saved >= 3072 + static_cast<int64_t>(a.M) * a.q_heads;
+}
+
 AttendPlan plan_attention(const AttendArgs& a) {
   AttendPlan p;
   const int64_t rows = static_cast<int64_t>(a.max_rows) * a.group;
-  const bool apart = a.prefix_len > 0 && a.seqs > 1 && rows < 64;
+  const bool apart = prefix_apart(a);
   p.own = shape_launch(a, apart ? kOwn : kPrefixAndOwn, rows, apart ? 0 : a.prefix_len, a.max_kv, a.seqs);
   p.parts = p.own.parts;
   if (apart) {
@@ -899,22 +911,15 @@ template <int D, int BITS, int RT> static void launch_both(const AttendArgs& a, 
   else attend_both_kernel<D, BITS, RT, 4><<<grid, block, 0, st>>>(a, p.prefix, p.own, p.parts);
 }
 
-template <int D, int BITS> static void launch_one(const AttendArgs& a, const AttendLaunch& n, int parts, hipStream_t st) {
-  const dim3 grid(static_cast<unsigned>(n.grid)), block(64 * kWaves);
-  if (n.row_tiles == 0 && n.alone) attend_rows_kernel<D, BITS, 1><<<grid, block, 0, st>>>(a, n, parts);
-  else if (n.row_tiles == 0) attend_rows_kernel<D, BITS, 4><<<grid, block, 0, st>>>(a, n, parts);
-  else if (n.row_tiles == 1) attend_tile_kernel<D, BITS, 1><<<grid, block, 0, st>>>(a, n, parts);
-  else attend_tile_kernel<D, BITS, 2><<<grid, block, 0, st>>>(a, n, parts);
-}
-
 template <int D, int BITS> static int run(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
-  if (p.prefix.grid && p.own.row_tiles == 0) {
-    if (p.prefix.row_tiles == 1) launch_both<D, BITS, 1>(a, p, st);
-    else launch_both<D, BITS, 2>(a, p, st);
-  } else {
-    if (p.prefix.grid) launch_one<D, BITS>(a, p.prefix, p.parts, st);
-    launch_one<D, BITS>(a, p.own, p.parts, st);
-  }
+  const AttendLaunch& n = p.own;
+  const dim3 grid(static_cast<unsigned>(n.grid)), block(64 * kWaves);
+  if (p.prefix.grid && p.prefix.row_tiles == 1) launch_both<D, BITS, 1>(a, p, st);
+  else if (p.prefix.grid) launch_both<D, BITS, 2>(a, p, st);
+  else if (n.row_tiles == 0 && n.alone) attend_rows_kernel<D, BITS, 1><<<grid, block, 0, st>>>(a, n, p.parts);
+  else if (n.row_tiles == 0) attend_rows_kernel<D, BITS, 4><<<grid, block, 0, st>>>(a, n, p.parts);
+  else if (n.row_tiles == 1) attend_tile_kernel<D, BITS, 1><<<grid, block, 0, st>>>(a, n, p.parts);
+  else attend_tile_kernel<D, BITS, 2><<<grid, block, 0, st>>>(a, n, p.parts);
   const int64_t outputs = static_cast<int64_t>(a.M) * a.q_heads;
   if (p.parts > 16) attend_join_kernel<D, 4><<<static_cast<unsigned>(outputs), 64 * kWaves, 0, st>>>(a, p);
   else if (p.parts > 1) attend_join_kernel<D, 1><<<static_cast<unsigned>(ceil_div(outputs, kWaves)), 64 * kWaves, 0, st>>>(a, p);

@@ -63,7 +63,7 @@ def test_rope_refusals():
     assert B.lib().rosaq_rope(None, Z, X, 4, 256, 2, 128, Y, 256, None) == NULL
     assert _code(lambda: f(at=0)) == NULL and _code(lambda: f(x=0)) == NULL and _code(lambda: f(y=0)) == NULL
     assert _code(lambda: f(_angles(table=0))) == NULL
-    assert _code(lambda: f(M=0)) == SHAPE and _code(lambda: f(M=(1 << 20) + 1)) == SHAPE
+    assert _code(lambda: f(M=0)) == SHAPE and _code(lambda: f(M=(1 << 26) + 1)) == SHAPE       # M x heads
     assert _code(lambda: f(heads=0)) == SHAPE and _code(lambda: f(heads=4097, ldx=1 << 20, ldy=1 << 20)) == SHAPE
     assert _code(lambda: f(M=1 << 20, heads=256, ldx=1 << 20, ldy=1 << 20)) == SHAPE
     assert _code(lambda: f(dim=96)) == ARG
