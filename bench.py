@@ -230,7 +230,7 @@ def shape_sweep(torch, shapes, ms_override, reps, emit):
         del W16, w16
 
 
-def decode_workload(torch, steps, warmup, absorbed=False, chained_mlp=True):
+def decode_workload(torch, steps, warmup, absorbed=False, chained_mlp=True, context=0, cache_bits=4):
     """The linears of a LLaMA-7B-shaped decode step at batch 64, INT4 g128, K = 128: per layer
     q/k/v (one batched call, shared head-wise rotation), o (head-wise), gate/up (one batched call
     sharing one dense 4096 x 4096 rotation) and down (no rotation, the paper's setting for W_D);
@@ -238,7 +238,9 @@ def decode_workload(torch, steps, warmup, absorbed=False, chained_mlp=True):
     the three FFN linears are one rosaq_mlp_swiglu call (the gated product goes straight into the down
     projection's input fragments); without it, rosaq_linear_swiglu and rosaq_linear(down) on a buffer
     of the same shape.  Returns a dict with the time per step next to the same linears as fp16
-    torch.matmul calls."""
+    torch.matmul calls.  With `context` tokens per sequence the step is also timed with what lies between
+    q/k/v and o: rotary positions and the new tokens' keys and values to a cache of `cache_bits` bits
+    (rosaq_cache_append), attention over the cache (rosaq_attention), every layer its own cache."""
     from paper_2506_13472_amd import binding as B, synth, torch_glue as T
     dev = torch.device("cuda:0")
     timer = Timer(torch, torch.cuda.Stream())
@@ -290,6 +292,33 @@ def decode_workload(torch, steps, warmup, absorbed=False, chained_mlp=True):
                                       y_f[0].stride(0), ws.data_ptr(), ws.numel(), sp)
                 T.linear(lay["down"], xh, y_d[3], ws)
 
+    def step_with_attention():
+        sp = T.current_stream_ptr()
+        for l, lay in enumerate(layers):
+            B.rosaq_linear_batch(qkv[l], x.data_ptr(), M, x.stride(0), ws.data_ptr(), ws.numel(), sp)
+            T.cache_append(caches[l], slots, y_d[1], y_d[2], rope=rope, positions=positions, q=y_d[0], q_out=y_d[0])
+            T.attention(plans[l], y_d[0], lengths, pages, out=y_att)
+            T.linear(lay["o"], y_att, y_d[3], ws)
+            B.rosaq_mlp_swiglu(lay["gate"], lay["up"], lay["down"], x.data_ptr(), M, x.stride(0),
+                               y_d[3].data_ptr(), y_d[3].stride(0), ws.data_ptr(), ws.numel(), sp)
+
+    if context:
+        page = 64
+        per_seq = -(-context // page)
+        caches = [T.KvCache(d // 128, 128, cache_bits, page, M * per_seq) for _ in range(L)]
+        plans = [T.AttentionPlan(c, d // 128, M, max_kv=context) for c in caches]
+        rope = T.Rope(T.rope_table(context, 128))
+        pages = torch.randperm(M * per_seq, device=dev).to(torch.int32).view(M, per_seq)
+        lengths = torch.full((M,), context, dtype=torch.int32, device=dev)
+        positions = lengths - 1
+        y_att = torch.empty((M, d), dtype=torch.float16, device=dev)
+        every = (pages.long()[:, :, None] * page + torch.arange(page, device=dev)).flatten(1)[:, :context].contiguous()
+        slots = every[:, -1].contiguous()                       # this step's tokens; the others are synthetic
+        for c in caches:
+            kv = [torch.randn((M * context, d), device=dev).to(torch.float16) for _ in range(2)]
+            T.cache_append(c, every.flatten(), *kv)
+        del kv
+
     # fp16: the same seven linears per layer as separate vendor GEMMs, and with q/k/v and gate/up fused
     W_qkv = [torch.randn((3 * d, d), dtype=torch.float16, device=dev) * 0.02 for _ in range(L)]
     W_o = [torch.randn((d, d), dtype=torch.float16, device=dev) * 0.02 for _ in range(L)]
@@ -318,6 +347,7 @@ def decode_workload(torch, steps, warmup, absorbed=False, chained_mlp=True):
     B.rosaq_tune("stages", 2)
     t_gemm = timer.run(step, steps, warmup)
     B.rosaq_tune("stages", 3)
+    t_att = timer.run(step_with_attention, steps, warmup) if context else None
     t16f = timer.run(step16_fused, steps, warmup)
     t16s = timer.run(step16_separate, steps, warmup)
 
@@ -352,6 +382,14 @@ def decode_workload(torch, steps, warmup, absorbed=False, chained_mlp=True):
         "speedup_vs_fp16_fused": round(t16f["median"] / ms, 3),
         "speedup_vs_fp16_separate": round(t16s["median"] / ms, 3),
         "data": "synthetic"}
+    if context:
+        cache_bytes = 2 * M * context * (d // 128) * (16 * cache_bits + 4)
+        extra = t_att["median"] - ms
+        out["with_attention"] = {
+            "context": context, "cache_bits": cache_bits, "ms_per_step": round(t_att["median"], 4),
+            "tokens_per_s": round(M / (t_att["median"] * 1e-3), 1), "attention_ms_per_step": round(extra, 4),
+            "cache_GB_read_per_step": round(cache_bytes * L / 1e9, 3),
+            "attention_GBps": round(cache_bytes * L / extra / 1e6, 1)}
     for lay in layers:
         for h in lay.values():
             h.free()
@@ -385,6 +423,10 @@ def main():
                          "rotations folded into the producing layers offline, no rotation at run time)")
     ap.add_argument("--unchained-mlp", action="store_true",
                     help="with --decode: rosaq_linear_swiglu + rosaq_linear(down) instead of rosaq_mlp_swiglu")
+    ap.add_argument("--attention", type=int, default=0, metavar="TOKENS",
+                    help="with --decode: also time the step with rotary positions, a quantised cache and attention over "
+                         "this many tokens per sequence between the q/k/v and output projections")
+    ap.add_argument("--cache-bits", type=int, default=4, choices=[4, 8], help="with --attention: bits of the cache")
     ap.add_argument("--sweep-filter", default="", help="substring of the shape names to run")
     ap.add_argument("--sweep-m", default="", help="comma-separated M values replacing each shape's own list")
     ap.add_argument("--copy-calibration", type=int, default=0, metavar="MiB",
@@ -430,7 +472,8 @@ def main():
         shape_sweep(torch, shapes, ms, 20, lambda row: print(json.dumps(row), flush=True))
         return
     if args.decode:
-        print(json.dumps(decode_workload(torch, args.decode_steps, args.warmup, args.absorbed, not args.unchained_mlp)), flush=True)
+        print(json.dumps(decode_workload(torch, args.decode_steps, args.warmup, args.absorbed, not args.unchained_mlp,
+                                         args.attention, args.cache_bits)), flush=True)
         return
 
     # ---- synthetic layers: calibrate (PCA per head on the GPU), pack, all through the C ABI ------
