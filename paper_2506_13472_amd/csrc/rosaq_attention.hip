@@ -649,9 +649,6 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
           for (int i = 0; i < 4; ++i) score[b][t][i] = i < lim && !(hidden >> b & 1) ? score[b][t][i] : -INFINITY;
         }
     }
-    uint4 ahead[U];                    // the first two records' values, on their way while the probabilities are made
-#pragma unroll
-    for (int j = 0; j < U; ++j) ahead[j] = from.v[0][j][lane];
     float most[RT];
     bool over = false;
 #pragma unroll
@@ -693,7 +690,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
         }
 #pragma unroll
       for (int j = 0; j < U; ++j) {
-        const half8 f = as_h8(p == 0 ? ahead[j] : from.v[1][j][lane]);
+        const half8 f = as_h8(from.v[p][j][lane]);
 #pragma unroll
         for (int t = 0; t < RT; ++t) sum[t][j] = mfma16(f, prob[t], sum[t][j]);
       }

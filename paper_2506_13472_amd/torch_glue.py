@@ -66,9 +66,10 @@ _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.curre
 
 def _ld(name: str, x: torch.Tensor, rows: int, width: int) -> int:
     """The row stride of an fp16 matrix [rows, width]; of a single row, whose stride torch leaves open, its width."""
-    if x.dtype is not _HALF or x.dim() != 2 or x.size(1) != width or x.size(0) != rows or x.stride(1) != 1:
+    stride = x.stride()
+    if x.dtype is not _HALF or x.shape != (rows, width) or stride[1] != 1:
         raise ValueError(f"{name} must be an fp16 tensor [{rows}, {width}] with unit column stride")
-    return x.stride(0) if rows > 1 else width
+    return stride[0] if rows > 1 else width
 
 
 def _integers(name: str, t: torch.Tensor, dtype: torch.dtype, count: int) -> int:
