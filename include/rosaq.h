@@ -351,7 +351,8 @@ int rosaq_cache_read(const rosaq_cache* cache, const int64_t* slots_dev, int32_t
  * Row i of a sequence of n rows and l cached tokens (the rows' own tokens among them, appended before) sees all of the prefix
  * and, of the sequence's tokens, all (causal 0) or those below l - n + i + 1 (causal 1).  A row that sees nothing is zero.
  * q_heads is a multiple of the cache's kv_heads: query head h reads kv head h / (q_heads / kv_heads).
- * Scores, sums and the softmax's statistics are fp32, probabilities are rounded to fp16 for their product with the values, y once. */
+ * Scores, sums and the softmax's statistics are fp32; a probability times the scale of its token's values is rounded to fp16 once for the
+ * product with their codes, and y once. */
 typedef struct {
   const rosaq_cache* cache;
   int32_t q_heads;

@@ -1,7 +1,8 @@
 // Attention over the quantised cache: y = softmax(scale q K^T) V with the keys and values as codes.
 //
-// One pass over the cache with the running reference and sum of a softmax.  A wave multiplies 16 query rows with 32 tokens a
-// step.  Both products run with the tokens on the rows of the MFMA's result, S^T = K Q^T and Y^T = V^T P^T:
+// One pass over the cache with the running reference and sum of a softmax, in two kernels: attend_rows for up to 16 rows of a sequence and
+// kv head (decode, drafted tokens), bound by the codes' way from memory, and attend_tile for more (prompts, a prefix under a whole
+// batch), bound by arithmetic.  Both products of both run with the tokens on the rows of the MFMA's result, S^T = K Q^T and Y^T = V^T P^T:
 // lane (g, r) of S^T holds query row r's scores of tokens 4 g .. 4 g + 3 of each 16, which is, as it stands, the operand P^T of
 // the second product if V's lanes bring the same tokens in the same order, and the cache's layout sees to that.  So the
 // probabilities go from one product to the other without leaving their registers, a row's reference and sum live in the
@@ -18,12 +19,14 @@ namespace rosaq {
 
 constexpr int kStep = 2 * kCacheBlock;      // tokens of a step: the depth of one MFMA over the values
 constexpr int kWaves = 4;
-constexpr int kRows = 16;                   // query rows of a workgroup
+constexpr int kRows = 16;                   // query rows of a tile of attend_rows
 constexpr float kNoScore = -1e30f;          // the reference before any score: finite, so that exp2(x - reference) is 0 or huge, never NaN, for hidden tokens
 
-// Probabilities are 2^(score - reference), kept in fp16 for the MFMA.  The reference is kLead below the largest score of
-// the step that set it, and moves only when a score passes it by kRoom: moving it costs shuffles and a pass over the sums, and hardly any
-// step needs it.  2^15 is in fp16's range, and what is 2^-24 below the reference (29 below the maximum, as powers of two) is lost.
+// What the second product multiplies are P' = fp16(2^(score - reference) s), with s the scale of the token's values: one rounding, to nearest, for a
+// product of three numbers, and no operation for the scale on each of the values.  The reference is of the same numbers: kLead
+// below the largest exponent of the step that set it, and it moves only when one passes it by kRoom, because moving it costs shuffles and a pass
+// over the sums and hardly any step needs it.  2^15 is in fp16's range; what is 2^-24 of the reference (2^-29 of the largest) is
+// lost to the product, and only to it: the sums of the probabilities are fp32, from before the rounding.
 constexpr float kLead = 5.f, kRoom = 15.f;
 
 // A sequence's rows in the call.
@@ -197,12 +200,14 @@ template <int D, int BITS> struct Step {
   int hidden;               // which of the two records have no page
 };
 
-// Few rows.  A wave takes one tile of up to 16 rows, alone (SPLIT 1: four tiles a workgroup) or as one of the four of a workgroup that take its
-// steps in turn (SPLIT 4) and add up what they have in LDS.
+// ---- few rows -----------------------------------------------------------------------------------
 //
-// Values enter the product as the whole numbers code - z and their scale s in the other factor, P' = fp16(p s): one rounding for
-// a product of three numbers, and an operation less for each of the values, which with so few rows is where the time goes.  So
-// that P' is in fp16's range whatever the scales are, the reference is one of p s, not of p; the sum of p is fp32.
+// A wave takes one tile of up to 16 rows and steps of 32 tokens, alone (SPLIT 1: four tiles a workgroup) or as one of the four of a workgroup
+// that take its steps in turn (SPLIT 4) and add up what they have in LDS.  Codes become factors in the registers they were loaded to, a step ahead,
+// their pages two.  Besides the stream of codes (5.3 TB/s of 5.2 that a copy reaches: 98 us for 65537 tokens x 32 heads of 8 bits)
+// the vector units bound it: some 270 operations a step and wave, of which those on 4-bit codes are as many as on 8-bit ones,
+// so that 4 bits reach 4.3 TB/s (88 us, 16 sequences of 8192 to 32768 tokens x 8 kv heads).  Short sequences are bound by the way to the
+// first codes (arguments, lengths, pages): 64 x 32 heads of up to 256 tokens take 17 us for 54 MB.
 template <int D> struct RowsLds {
   float sum[kWaves][kRows][D + 4];
   float ref[kWaves][kRows], l[kWaves][kRows];
@@ -418,7 +423,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const AttendLau
 
 // ---- many rows ----------------------------------------------------------------------------------
 //
-// A workgroup of four waves takes 64 RT query rows of one sequence and kv head (of all rows of the call, over the prefix) and
+// A workgroup of four waves takes 64 RT query rows (RT 1 for up to 64 rows, else 2) of one sequence and kv head (of all rows of the call, over the prefix) and
 // stages of 64 tokens.  The codes become fp16 factors once a stage, a record's keys and half of two records' values a wave, and go to LDS as whole MFMA
 // operands (1 KiB, lane order), which all waves read.
 // Both are the whole numbers code - z.  The keys' scale acts on the scores, in fp32: rounded factors would be off by 2^-11 of a
@@ -426,6 +431,13 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const AttendLau
 // with log2 s over the keys' scale as what the sum of a score starts from.
 // The sum of the probabilities, P' / s in fp32, takes P' before it is rounded: next to a token of large values, those of others may round to nothing,
 // which the product does not notice, but their weights would be missing here.
+//
+// Measured: four prompts of 2048 tokens x 32 heads (8 bits) 180 us = 766 TFLOP/s of the products that the mask leaves (a product of two
+// 8192 x 8192 fp16 matrices: 1133).  The matrix cores are busy 31 % of that; a stage of a wave takes 64 MFMAs of 16 cycles beside some 230 vector
+// operations (four cycles; sixteen for each of its 32 exponentials) and 32 KiB out of LDS, one stage after the other in each wave, and two waves a SIMD (240 registers) overlap
+// about half.  Built and slower: eight waves a workgroup with half of them half a stage behind (233 against 189 us: the barriers
+// cost more than the sharing saves), the factors of the next stage between the MFMAs by the scheduler's groups (spills; 260
+// against 239 on the 4-bit chunk), three and four row tiles a wave (spills), priorities around either product (none or worse).
 constexpr int kStage = 4 * kCacheBlock;
 
 template <int D, int BITS> struct StageCodes {
@@ -856,6 +868,15 @@ __global__ __launch_bounds__(64 * kWaves) void attend_join_kernel(AttendArgs a, 
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Shapes a launch over `rows` rows and `tokens` tokens of each of `seqs` sequences.
+//
+// Kernel: up to 16 rows are one tile of attend_rows.  From 17 to 32 both are as fast (us, attend_tile / attend_rows: 8 sequences of up to 8192 tokens x 8
+// kv heads, 32 rows, 4 bits 41 / 38; 32 of up to 1024, 8 bits 28 / 29; one of 32768 27 / 30), at 48 rows attend_tile is (43 / 45, 33 / 48, 30 / 49).
+// Parts: enough workgroups for all compute units, eight steps or two stages in each at least.  More of them balance ragged lengths better and cost more
+// partial results: 16 sequences of 8192 to 32768 tokens in 1536 / 2048 / 3072 / 6144 workgroups 96 / 89 / 89 / 93 us; a chunk of 3 x 509 rows x 32 heads,
+// 384 workgroups as they are 239 us, in 2, 3, 4 and 5 parts 292, 240, 286 and 224: which is best goes by the lengths, which the host does not
+// know.  A prefix under 64 rows, 32 heads: 256 / 512 workgroups 27.6 / 32.2 us beside the sequences' own.
+// Waves alone: where there are 2048 tiles of up to 16 steps (64 x 32 heads, us together / alone: 256 tokens 20.6 / 19.3, 512 34.2 / 32.3, 1024
+// 52.5 / 54.8).
 static AttendLaunch shape_launch(const AttendArgs& a, int over, int64_t rows, int64_t tokens_prefix, int64_t tokens_own, int64_t seqs) {
   AttendLaunch n;
   n.over = over;
