@@ -98,19 +98,19 @@ static int check_rope(const rosaq_rope_angles* r, const int32_t* positions, int3
   return ROSAQ_OK;
 }
 
-// Whether two matrices share elements.  With one leading dimension they may be columns of one buffer.
-static bool overlap(const void* x, int64_t ldx, const void* y, int64_t ldy, int M, int64_t width) {
-  const uintptr_t x0 = reinterpret_cast<uintptr_t>(x), x1 = x0 + 2 * (static_cast<uint64_t>(M - 1) * ldx + width);
-  const uintptr_t y0 = reinterpret_cast<uintptr_t>(y), y1 = y0 + 2 * (static_cast<uint64_t>(M - 1) * ldy + width);
+// Whether two matrices of M rows share elements.  With one leading dimension they may be columns of one buffer.
+static bool overlap(const void* x, int64_t ldx, int64_t wx, const void* y, int64_t ldy, int64_t wy, int M) {
+  const uintptr_t x0 = reinterpret_cast<uintptr_t>(x), x1 = x0 + 2 * (static_cast<uint64_t>(M - 1) * ldx + wx);
+  const uintptr_t y0 = reinterpret_cast<uintptr_t>(y), y1 = y0 + 2 * (static_cast<uint64_t>(M - 1) * ldy + wy);
   if (!(x0 < y1 && y0 < x1)) return false;
   if (ldx != ldy) return true;
-  const uint64_t row = 2 * static_cast<uint64_t>(ldx), w = 2 * static_cast<uint64_t>(width);
-  const uint64_t at = y0 >= x0 ? (y0 - x0) % row : (row - (x0 - y0) % row) % row;
-  return !(at >= w && at + w <= row);
+  const uint64_t row = 2 * static_cast<uint64_t>(ldx);
+  const uint64_t at = y0 >= x0 ? (y0 - x0) % row : (row - (x0 - y0) % row) % row;     // of y's rows within x's
+  return !(at >= 2 * static_cast<uint64_t>(wx) && at + 2 * static_cast<uint64_t>(wy) <= row);
 }
 static int check_in_place(const void* x, int64_t ldx, const void* y, int64_t ldy, int M, int64_t width) {
   if (x == y && ldx == ldy) return ROSAQ_OK;
-  return overlap(x, ldx, y, ldy, M, width) ? fail(ROSAQ_ERR_ARG, "the output overlaps the input without being the same matrix") : ROSAQ_OK;
+  return overlap(x, ldx, width, y, ldy, width, M) ? fail(ROSAQ_ERR_ARG, "the output overlaps the input without being the same matrix") : ROSAQ_OK;
 }
 
 static int check_attention(const rosaq_attention_desc* d, AttendArgs* a, bool pointers) {
@@ -140,7 +140,7 @@ static int check_attention(const rosaq_attention_desc* d, AttendArgs* a, bool po
   if (pointers) {
     if ((rc = check_matrix("q", d->q_dev, d->ldq, width)) != ROSAQ_OK) return rc;
     if ((rc = check_matrix("y", d->y_dev, d->ldy, width)) != ROSAQ_OK) return rc;
-    if (overlap(d->q_dev, d->ldq, d->y_dev, d->ldy, d->M, width)) return fail(ROSAQ_ERR_ARG, "y must not overlap q");
+    if (overlap(d->q_dev, d->ldq, width, d->y_dev, d->ldy, width, d->M)) return fail(ROSAQ_ERR_ARG, "y must not overlap q");
     if (!d->kv_len_dev) return fail(ROSAQ_ERR_NULL, "kv_len_dev is NULL");
     if (d->max_kv > 0 && !d->pages_dev) return fail(ROSAQ_ERR_NULL, "pages_dev is NULL");
     if (d->prefix_len > 0 && !d->prefix_pages_dev) return fail(ROSAQ_ERR_NULL, "prefix_pages_dev is NULL");
@@ -230,7 +230,12 @@ int rosaq_cache_append(const rosaq_cache* cache, const int64_t* slots_dev, int32
     heads += q_heads;
   }
   if ((rc = check_rows(M, heads)) != ROSAQ_OK) return rc;
-  if (q_dev && (rc = check_in_place(q_dev, ldq, q_out_dev, ldq_out, M, static_cast<int64_t>(q_heads) * cache->head_dim)) != ROSAQ_OK) return rc;
+  if (q_dev) {
+    const int64_t q_width = static_cast<int64_t>(q_heads) * cache->head_dim;
+    if ((rc = check_in_place(q_dev, ldq, q_out_dev, ldq_out, M, q_width)) != ROSAQ_OK) return rc;
+    if (overlap(k_dev, ldk, width, q_out_dev, ldq_out, q_width, M) || overlap(v_dev, ldv, width, q_out_dev, ldq_out, q_width, M))
+      return fail(ROSAQ_ERR_ARG, "q_out must not overlap k or v");
+  }
   a.slots = slots_dev; a.M = M; a.k = k_dev; a.ldk = ldk; a.v = v_dev; a.ldv = ldv;
   a.q = q_dev; a.ldq = ldq; a.q_heads = q_dev ? q_heads : 0; a.q_out = q_out_dev; a.ldq_out = ldq_out;
   a.dim = cache->head_dim; a.bits = cache->bits;
@@ -248,6 +253,7 @@ int rosaq_cache_read(const rosaq_cache* cache, const int64_t* slots_dev, int32_t
   if ((k_dev && (rc = check_matrix("k", k_dev, ldk, width)) != ROSAQ_OK) || (v_dev && (rc = check_matrix("v", v_dev, ldv, width)) != ROSAQ_OK))
     return rc;
   if ((rc = check_rows(M, 2 * static_cast<int64_t>(cache->kv_heads))) != ROSAQ_OK) return rc;
+  if (k_dev && v_dev && overlap(k_dev, ldk, width, v_dev, ldv, width, M)) return fail(ROSAQ_ERR_ARG, "k and v must not overlap");
   a.slots = slots_dev; a.M = M; a.k = k_dev; a.ldk = ldk; a.v = v_dev; a.ldv = ldv; a.dim = cache->head_dim; a.bits = cache->bits;
   return launch_cache_read(a, hip_stream);
 }

@@ -943,7 +943,7 @@ template <int D, int BITS> static int run(const AttendArgs& a, const AttendPlan&
   else if (p.parts > 1) attend_join_kernel<D, 1><<<static_cast<unsigned>(ceil_div(outputs, kWaves)), 64 * kWaves, 0, st>>>(a, p);
   const hipError_t e = hipGetLastError();
   if (e == hipSuccess) return ROSAQ_OK;
-  set_error(std::string("attention: ") + hipGetErrorString(e));
+  try { set_error(std::string("attention: ") + hipGetErrorString(e)); } catch (...) {}     // no memory for the text
   return ROSAQ_ERR_HIP;
 }
 

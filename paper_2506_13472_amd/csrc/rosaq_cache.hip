@@ -17,7 +17,7 @@ namespace rosaq {
 static int launched(const char* what) {
   const hipError_t e = hipGetLastError();
   if (e == hipSuccess) return ROSAQ_OK;
-  set_error(std::string(what) + ": " + hipGetErrorString(e));
+  try { set_error(std::string(what) + ": " + hipGetErrorString(e)); } catch (...) {}     // no memory for the text
   return ROSAQ_ERR_HIP;
 }
 
