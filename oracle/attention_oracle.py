@@ -66,7 +66,7 @@ def values(code, s, z) -> np.ndarray:
 
 def held(x: np.ndarray, heads: int, bits: int) -> np.ndarray:
     """fp64 [M, heads, d]: what the cache holds of fp16 x [M, heads * d]."""
-    return values(*quantise(x.reshape(x.shape[0], heads, -1), bits))
+    return values(*quantise(x.reshape(x.shape[0], heads, x.shape[1] // heads), bits))
 
 
 def attention(q, k, v, limits, scale):

@@ -161,6 +161,19 @@ def test_append_odd_groups(bits, dim):
     assert np.isfinite(want[2:4]).all()
 
 
+def test_more_than_a_million_tokens():
+    print("case many tokens", flush=True)
+    M = (1 << 20) + 37
+    g = torch.Generator(device="cuda").manual_seed(4)
+    k, v = (torch.randn((M, 64), generator=g, device="cuda").to(torch.float16) for _ in range(2))
+    cache = T.KvCache(1, 64, 4, 64, M // 64 + 1)
+    slots = torch.randperm(cache.num_pages * 64, generator=g, device="cuda")[:M]
+    T.cache_append(cache, slots, k, v)
+    some = torch.cat([torch.arange(M - 100, M, device="cuda"), torch.randint(0, M, (2000,), generator=g, device="cuda")])
+    for got, x in zip(T.cache_read(cache, slots), (k, v)):
+        same_bits(got[some], A.held(x[some].cpu().numpy(), 1, 4).astype(np.float16).reshape(len(some), -1))
+
+
 def test_append_skips_tokens_without_slot_or_position():
     print("case cache skipped tokens", flush=True)
     rng = np.random.default_rng(3)
@@ -305,6 +318,31 @@ def test_shared_prefix(bits, prefix, lens, rows, kv, group, dim):
     y = b.run()
     b.check(y)
     assert torch.equal(y, b.run())
+
+
+def _spread(n, top, seed):
+    return [int(x) for x in np.random.default_rng(seed).integers(0, top + 1, n)]
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("prefix,lens,rows,kv,group,dim", [(2100, _spread(40, 90, 1), [1] * 40, 2, 1, 128), (2075, _spread(60, 40, 2), [1] * 60, 2, 1, 64),
+                                                           (3001, _spread(40, 70, 3), _spread(40, 3, 4), 1, 4, 128), (5000, _spread(24, 9, 5), [2] * 24, 1, 8, 64),
+                                                           (200, _spread(64, 40, 6), [1] * 64, 32, 1, 64), (130, _spread(64, 33, 7), [1] * 64, 32, 2, 64),
+                                                           (161, _spread(64, 5, 8), [1] * 64, 32, 1, 128), (150, [0] * 70, [1] * 70, 32, 2, 128)])
+def test_prefix_computed_once_for_all(bits, prefix, lens, rows, kv, group, dim):
+    """Batches that save enough by it: up to 64 rows of a kv head and more, few and many heads, some of the sequences without tokens or rows."""
+    print(f"case apart int{bits} {prefix} {len(lens)} sequences heads {kv} x {group} dim {dim}", flush=True)
+    b = Batch(prefix + bits, lens, rows, kv, group, dim, bits, 32, prefix=prefix, pad=2)
+    plan = b.plan()
+    assert plan.ws_bytes >= 2 * b.M * kv * group * (dim + 2) * 4       # at least two parts: the prefix, the sequences' own
+    b.append()
+    y = b.run(plan)
+    b.check(y)
+    assert torch.equal(y, b.run(plan))
+    b.prefix_table[1] = -1                                              # a page of the prefix that is none
+    hidden = np.zeros(len(b.slots), bool)
+    hidden[32:64] = True
+    b.check(b.run(plan), hidden)
 
 
 @pytest.mark.parametrize("prefix,rows", [(0, 1), (0, 3), (70, 1), (70, 3), (0, 150)])
