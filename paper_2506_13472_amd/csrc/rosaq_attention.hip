@@ -872,7 +872,7 @@ static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // Kernel: up to 16 rows are one tile of attend_rows.  From 17 to 32 both are as fast (us, attend_tile / attend_rows: 8 sequences of up to 8192 tokens x 8
 // kv heads, 32 rows, 4 bits 41 / 38; 32 of up to 1024, 8 bits 28 / 29; one of 32768 27 / 30), at 48 rows attend_tile is (43 / 45, 33 / 48, 30 / 49).
 // Parts: enough workgroups for all compute units, eight steps or two stages in each at least.  More of them balance ragged lengths better and cost more
-// partial results: 16 sequences of 8192 to 32768 tokens in 1536 / 2048 / 3072 / 6144 workgroups 96 / 89 / 89 / 93 us; a chunk of 3 x 509 rows x 32 heads,
+// partial results: 16 sequences of 8192 to 32768 tokens in 1536 / 2048 / 2560 / 6144 workgroups 96 / 89 / 89 / 93 us; a chunk of 3 x 509 rows x 32 heads,
 // 384 workgroups as they are 239 us, in 2, 3, 4 and 5 parts 292, 240, 286 and 224: which is best goes by the lengths, which the host does not
 // know.  A prefix under 64 rows, 32 heads: 256 / 512 workgroups 27.6 / 32.2 us beside the sequences' own.
 // Waves alone: where there are 2048 tiles of up to 16 steps (64 x 32 heads, us together / alone: 256 tokens 20.6 / 19.3, 512 34.2 / 32.3, 1024
@@ -905,7 +905,7 @@ static AttendLaunch shape_launch(const AttendArgs& a, int over, int64_t rows, in
 static bool prefix_apart(const AttendArgs& a) {
   if (a.prefix_len == 0 || a.max_rows * static_cast<int64_t>(a.group) > kRows) return false;
   const int64_t saved = static_cast<int64_t>(a.seqs - 1) * a.cache.kv_heads * ceil_div(a.prefix_len, kStep);
-  return saved >= 3072 + static_cast<int64_t>(a.M) * a.q_heads;
+  return saved >= 3000 + static_cast<int64_t>(a.M) * a.q_heads;
 }
 
 AttendPlan plan_attention(const AttendArgs& a) {

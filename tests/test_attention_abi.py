@@ -98,7 +98,7 @@ def test_append_refusals():
     assert _code(lambda: f(**r, **dict(q, q_ptr=Z, q_out_ptr=X + 512))) == ARG                # over k, over v
     assert _code(lambda: f(**r, **dict(q, q_ptr=Z, q_out_ptr=Y - 1024))) == ARG
     # columns of one buffer, q turned in place: apart, so that the call gets to its next complaint
-    one = dict(k=X + 2048, ldk=2048, v=X + 3072, ldv=2048, **r, **dict(q, q_ptr=X, q_out_ptr=X, ldq=2048, ldq_out=2048))
+    one = dict(k=X + 2048, ldk=2048, v=X + 3200, ldv=2048, **r, **dict(q, q_ptr=X, q_out_ptr=X, ldq=2048, ldq_out=2048))
     assert _code(lambda: f(M=1 << 25, **one)) == SHAPE
     assert _code(lambda: f(**dict(one, q_heads=9, ldq=2048))) == ARG                          # q's last head is k's first
     assert _code(lambda: f(M=1 << 20, **r, **dict(q, q_heads=125, ldq=1 << 15, ldq_out=1 << 15))) == SHAPE
