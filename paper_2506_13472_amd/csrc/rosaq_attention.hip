@@ -221,12 +221,24 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const AttendLau
   const Share w = share_of(a, n, SPLIT == 1 ? block * kWaves + wave : block);
   if (!w.any) return;
   const int kv_head = w.kv_head, seq = w.seq, tile = w.tile;
+  const CacheDev& c = a.cache;
+  const int block_shift = c.page_shift - 4;
+  const char* head_base = c.base + kv_head * c.head_bytes;
+  const int32_t* own_pages = a.pages + static_cast<int64_t>(seq) * a.page_stride;
+  const int prefix_steps = prefix_steps_of(a, n.over, kStep);
+  // pages of a step, given how many tokens the sequence has
+  auto pages_of = [&](int step, int tokens) {
+    const bool own = step >= prefix_steps;
+    return look_up<2>(own ? own_pages : a.prefix_pages, (own ? step - prefix_steps : step) * 2,
+                      ((own ? tokens : a.prefix_len) + kCacheBlock - 1) / kCacheBlock, block_shift);
+  };
+  // those of the first step are fetched beside the sequence's length, for as many tokens as it may have
+  const Pages<2> first_pages = pages_of(w.part * n.steps + (SPLIT == 1 ? 0 : wave), a.capacity);
   const Rows rows = rows_of(a, seq);
   const int used = min(rows.count, a.max_rows) * a.group;         // rows of this kv head: (token, query head of the group)
   if (tile * kRows >= used) return;
   const int tokens = own_tokens(a, seq);
   const int first = tile * kRows / a.group, last = (min(tile * kRows + kRows, used) - 1) / a.group;
-  const int prefix_steps = prefix_steps_of(a, n.over, kStep);
   const int all = steps_of(a, n.over, kStep, tokens, rows.count, last);
   const int begin = w.part * n.steps, end = min(begin + n.steps, all);
   if (w.part > 0 && begin >= all) return;                         // part 0 always answers, if only that there is nothing
@@ -236,27 +248,6 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const AttendLau
   const int my_token = my / a.group;
   const int limit = visible(a, tokens, rows.count, my_token), least = visible(a, tokens, rows.count, first);
 
-  half8 q[KS];
-  {
-    const _Float16* src = static_cast<const _Float16*>(a.q) + static_cast<int64_t>(rows.start + my_token) * a.ldq +
-                          (kv_head * a.group + my % a.group) * D + g * (D / 4);
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      const half8 h = as_h8(reinterpret_cast<const uint4*>(src)[s]);
-      q[s] = BITS == 4 ? half8{h[0], h[4], h[1], h[5], h[2], h[6], h[3], h[7]} : h;
-    }
-  }
-
-  const CacheDev& c = a.cache;
-  const int block_shift = c.page_shift - 4;
-  const char* head_base = c.base + kv_head * c.head_bytes;
-  const int32_t* own_pages = a.pages + static_cast<int64_t>(seq) * a.page_stride;
-
-  auto pages_of = [&](int step) {
-    const bool own = step >= prefix_steps;
-    return look_up<2>(own ? own_pages : a.prefix_pages, (own ? step - prefix_steps : step) * 2,
-                      step < end ? ((own ? tokens : a.prefix_len) + kCacheBlock - 1) / kCacheBlock : 0, block_shift);
-  };
   auto load = [&](int step, const Pages<2>& pages, Step<D, BITS>& x) {
     int64_t at[2];
     x.hidden = place<2>(c, pages, (step >= prefix_steps ? step - prefix_steps : step) * 2, block_shift, kRecord, at);
@@ -271,6 +262,24 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const AttendLau
       x.v_sz[b] = reinterpret_cast<const uint4*>(sz)[4 + g];
     }
   };
+
+  // The first codes are asked for first: the queries' way is as long.
+  constexpr int kTurn = SPLIT == 1 ? 1 : kWaves;
+  int step = begin + (SPLIT == 1 ? 0 : wave);
+  Step<D, BITS> x, y;
+  if (step < end) load(step, first_pages, x);
+  auto tokens_to = [&](int step) { return step < end ? tokens : 0; };
+
+  half8 q[KS];
+  {
+    const _Float16* src = static_cast<const _Float16*>(a.q) + static_cast<int64_t>(rows.start + my_token) * a.ldq +
+                          (kv_head * a.group + my % a.group) * D + g * (D / 4);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const half8 h = as_h8(reinterpret_cast<const uint4*>(src)[s]);
+      q[s] = BITS == 4 ? half8{h[0], h[4], h[1], h[5], h[2], h[6], h[3], h[7]} : h;
+    }
+  }
 
   floatx4 sum[U];
 #pragma unroll
@@ -346,25 +355,20 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const AttendLau
     }
   };
 
-  constexpr int kTurn = SPLIT == 1 ? 1 : kWaves;
-  int step = begin + (SPLIT == 1 ? 0 : wave);
   if (step < end) {
     // two steps' codes: one is multiplied while the next is on its way, and the pages of the one after
-    Step<D, BITS> x, y;
-    Pages<2> next = pages_of(step);
-    load(step, next, x);
-    next = pages_of(step + kTurn);
+    Pages<2> next = pages_of(step + kTurn, tokens_to(step + kTurn));
     while (true) {
       if (step + kTurn < end) {
         load(step + kTurn, next, y);
-        next = pages_of(step + 2 * kTurn);
+        next = pages_of(step + 2 * kTurn, tokens_to(step + 2 * kTurn));
       }
       multiply(step, x);
       step += kTurn;
       if (step >= end) break;
       if (step + kTurn < end) {
         load(step + kTurn, next, x);
-        next = pages_of(step + 2 * kTurn);
+        next = pages_of(step + 2 * kTurn, tokens_to(step + 2 * kTurn));
       }
       multiply(step, y);
       step += kTurn;
@@ -492,21 +496,6 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
   const bool idle = first_row >= used;                            // it still brings its share of the codes
   const int least = visible(a, tokens, rows.count, min(first_row, used - 1) / a.group);
   const int most_seen = visible(a, tokens, rows.count, min(first_row + 16 * RT - 1, used - 1) / a.group);
-  half8 q[RT][KS];
-  int limit[RT];
-#pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    const int my = min(first_row + 16 * t + r, used - 1), my_token = my / a.group;
-    limit[t] = visible(a, tokens, rows.count, my_token);
-    const _Float16* src = static_cast<const _Float16*>(a.q) + static_cast<int64_t>(rows.start + my_token) * a.ldq +
-                          (w.kv_head * a.group + my % a.group) * D + g * (D / 4);
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      const half8 h = as_h8(reinterpret_cast<const uint4*>(src)[s]);
-      q[t][s] = BITS == 4 ? half8{h[0], h[4], h[1], h[5], h[2], h[6], h[3], h[7]} : h;
-    }
-  }
-
   const CacheDev& c = a.cache;
   const int block_shift = c.page_shift - 4;
   const char* head_base = c.base + w.kv_head * c.head_bytes;
@@ -613,6 +602,24 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
     }
   };
 
+  Codes x;
+  const Pages<4> first_pages = pages_of(begin);
+  if (begin < end) load(begin, first_pages, x);       // first, as in attend_rows
+  half8 q[RT][KS];
+  int limit[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const int my = min(first_row + 16 * t + r, used - 1), my_token = my / a.group;
+    limit[t] = visible(a, tokens, rows.count, my_token);
+    const _Float16* src = static_cast<const _Float16*>(a.q) + static_cast<int64_t>(rows.start + my_token) * a.ldq +
+                          (w.kv_head * a.group + my % a.group) * D + g * (D / 4);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const half8 h = as_h8(reinterpret_cast<const uint4*>(src)[s]);
+      q[t][s] = BITS == 4 ? half8{h[0], h[4], h[1], h[5], h[2], h[6], h[3], h[7]} : h;
+    }
+  }
+
   floatx4 sum[RT][U];
   float ref[RT], l[RT];
 #pragma unroll
@@ -710,11 +717,8 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
   };
 
   if (begin < end) {
-    Codes x;
     int hidden;
-    Pages<4> next = pages_of(begin);
-    load(begin, next, x);
-    next = pages_of(begin + 1);
+    Pages<4> next = pages_of(begin + 1);
     store(begin, x, lds[0]);
     hidden = x.hidden;
     lds_barrier();
