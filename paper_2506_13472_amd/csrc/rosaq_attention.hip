@@ -207,7 +207,7 @@ template <int D, int BITS> struct Step {
 // their pages two.  Besides the stream of codes (5.3 TB/s of 5.2 that a copy reaches: 98 us for 65537 tokens x 32 heads of 8 bits)
 // the vector units bound it: some 270 operations a step and wave, of which those on 4-bit codes are as many as on 8-bit ones,
 // so that 4 bits reach 4.3 TB/s (88 us, 16 sequences of 8192 to 32768 tokens x 8 kv heads).  Short sequences are bound by the way to the
-// first codes (arguments, lengths, pages): 64 x 32 heads of up to 256 tokens take 17 us for 54 MB.
+// first codes (arguments, lengths, pages): 64 x 32 heads of up to 256 tokens take 16 us for 54 MB.
 template <int D> struct RowsLds {
   float sum[kWaves][kRows][D + 4];
   float ref[kWaves][kRows], l[kWaves][kRows];
@@ -436,12 +436,13 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const AttendLau
 // The sum of the probabilities, P' / s in fp32, takes P' before it is rounded: next to a token of large values, those of others may round to nothing,
 // which the product does not notice, but their weights would be missing here.
 //
-// Measured: four prompts of 2048 tokens x 32 heads (8 bits) 180 us = 766 TFLOP/s of the products that the mask leaves (a product of two
+// Measured: four prompts of 2048 tokens x 32 heads (8 bits) 180 to 186 us = 740 to 766 TFLOP/s of the products that the mask leaves (a product of two
 // 8192 x 8192 fp16 matrices: 1133).  The matrix cores are busy 31 % of that; a stage of a wave takes 64 MFMAs of 16 cycles beside some 230 vector
 // operations (four cycles; sixteen for each of its 32 exponentials) and 32 KiB out of LDS, one stage after the other in each wave, and two waves a SIMD (240 registers) overlap
 // about half.  Built and slower: eight waves a workgroup with half of them half a stage behind (233 against 189 us: the barriers
 // cost more than the sharing saves), the factors of the next stage between the MFMAs by the scheduler's groups (spills; 260
-// against 239 on the 4-bit chunk), three and four row tiles a wave (spills), priorities around either product (none or worse).
+// against 239 on the 4-bit chunk), three and four row tiles a wave (spills), half a stage at a time and one stage's LDS for three workgroups
+// a unit (spills), priorities around either product (none or worse), the first codes before the queries (188 against 186).
 constexpr int kStage = 4 * kCacheBlock;
 
 template <int D, int BITS> struct StageCodes {
@@ -496,6 +497,21 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
   const bool idle = first_row >= used;                            // it still brings its share of the codes
   const int least = visible(a, tokens, rows.count, min(first_row, used - 1) / a.group);
   const int most_seen = visible(a, tokens, rows.count, min(first_row + 16 * RT - 1, used - 1) / a.group);
+  half8 q[RT][KS];
+  int limit[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const int my = min(first_row + 16 * t + r, used - 1), my_token = my / a.group;
+    limit[t] = visible(a, tokens, rows.count, my_token);
+    const _Float16* src = static_cast<const _Float16*>(a.q) + static_cast<int64_t>(rows.start + my_token) * a.ldq +
+                          (w.kv_head * a.group + my % a.group) * D + g * (D / 4);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const half8 h = as_h8(reinterpret_cast<const uint4*>(src)[s]);
+      q[t][s] = BITS == 4 ? half8{h[0], h[4], h[1], h[5], h[2], h[6], h[3], h[7]} : h;
+    }
+  }
+
   const CacheDev& c = a.cache;
   const int block_shift = c.page_shift - 4;
   const char* head_base = c.base + w.kv_head * c.head_bytes;
@@ -602,24 +618,6 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
     }
   };
 
-  Codes x;
-  const Pages<4> first_pages = pages_of(begin);
-  if (begin < end) load(begin, first_pages, x);       // first, as in attend_rows
-  half8 q[RT][KS];
-  int limit[RT];
-#pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    const int my = min(first_row + 16 * t + r, used - 1), my_token = my / a.group;
-    limit[t] = visible(a, tokens, rows.count, my_token);
-    const _Float16* src = static_cast<const _Float16*>(a.q) + static_cast<int64_t>(rows.start + my_token) * a.ldq +
-                          (w.kv_head * a.group + my % a.group) * D + g * (D / 4);
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      const half8 h = as_h8(reinterpret_cast<const uint4*>(src)[s]);
-      q[t][s] = BITS == 4 ? half8{h[0], h[4], h[1], h[5], h[2], h[6], h[3], h[7]} : h;
-    }
-  }
-
   floatx4 sum[RT][U];
   float ref[RT], l[RT];
 #pragma unroll
@@ -717,8 +715,11 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
   };
 
   if (begin < end) {
+    Codes x;
     int hidden;
-    Pages<4> next = pages_of(begin + 1);
+    Pages<4> next = pages_of(begin);
+    load(begin, next, x);
+    next = pages_of(begin + 1);
     store(begin, x, lds[0]);
     hidden = x.hidden;
     lds_barrier();
