@@ -545,6 +545,37 @@ def test_another_stream_and_a_graph():
             torch.randn(1000, device="cuda").sum().item()
 
 
+@pytest.mark.parametrize("lens,rows,kv,group,prefix", [(_spread(40, 90, 1), 1, 2, 1, 2100), ([5000, 3000], 1, 2, 2, 0), ([900], 300, 2, 2, 0)])
+def test_two_graphs_share_a_workspace(lens, rows, kv, group, prefix):
+    """Replayed in turn, with other work between: every call writes its partial results before it reads them."""
+    print(f"case two graphs {len(lens)} x {rows} prefix {prefix}", flush=True)
+    b = Batch(21, lens, [rows] * len(lens), kv, group, 128, 4, 64, prefix=prefix)
+    b.append()
+    plan, n, table, start = b.plan(), dev(np.array(lens, np.int32)), dev(b.table), dev(b.row_start)
+    pre = dev(b.prefix_table) if prefix else None
+    qs = [dev(b.q), dev(b.q[::-1].copy())]
+    ys = [torch.empty_like(q) for q in qs]
+    want = [T.attention(plan, q, n, table, row_start=start, prefix_pages=pre).clone() for q in qs]
+    b.check(want[0])
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    graphs = []
+    with torch.cuda.stream(side):
+        for q, y in zip(qs, ys):
+            graphs.append(torch.cuda.CUDAGraph())
+            with torch.cuda.graph(graphs[-1], stream=side):
+                T.attention(plan, q, n, table, row_start=start, prefix_pages=pre, out=y)
+    torch.cuda.synchronize()
+    for turn in range(3):
+        for i in (0, 1, 1, 0):
+            ys[i].zero_()
+            graphs[i].replay()
+            torch.cuda.synchronize()
+            assert torch.equal(ys[i], want[i]), (turn, i)
+            plan.ws.fill_(0xff)                          # what a call finds there is of no account
+            torch.randn(1000, device="cuda").sum().item()
+
+
 def test_two_plans_on_two_streams():
     print("case two streams", flush=True)
     b = Batch(17, [4000, 5000], [1, 1], 2, 2, 128, 8, 64)
