@@ -14,9 +14,9 @@ static int fail(int code, const char* msg) {
   return code;
 }
 
-// Launches number 16 tasks a workgroup of 256 threads, and a grid has fewer than 2^32 threads.
+// Rows x heads: what the launches of rotary positions and cache, with 16 of them a workgroup of 256 threads, number in 32 bits.
 constexpr int64_t kMaxTasks = int64_t{1} << 27;
-constexpr int64_t kMaxGrid = int64_t{1} << 24;
+constexpr int64_t kMaxGrid = int64_t{1} << 24;     // workgroups of 256 threads, of which a dimension of a grid has fewer than 2^32
 constexpr int kMaxSequences = 1 << 20;
 
 static bool misaligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n != 0; }

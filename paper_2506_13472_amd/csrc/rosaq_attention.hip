@@ -771,12 +771,15 @@ __global__ __launch_bounds__(64 * kWaves, RT == 1 && BITS == 4 ? 3 : 2) void att
 
 // Adds up the parts of one (row, head): those of its own tokens that its sequence is long enough for, and all of the prefix.  WAVES of a workgroup of
 // four take one: parts go to its half waves in turn, 4 (D 64: 2) channels a lane, and a half wave's loads do not wait for each other.
+// A call may have 2^27 outputs, and a dimension of a grid ends at 2^32 threads, beyond which a launch runs a part of them without an error: the
+// workgroups lie in rows of kJoinRow.
+constexpr int kJoinRow = 1 << 20;
 template <int D, int WAVES>
 __global__ __launch_bounds__(64 * kWaves) void attend_join_kernel(AttendArgs a, AttendPlan plan) {
   constexpr int C = D / 32, kHalves = 2 * WAVES;
   typedef float vec __attribute__((ext_vector_type(C)));
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t task = WAVES == 1 ? static_cast<int64_t>(blockIdx.x) * kWaves + wave : static_cast<int64_t>(blockIdx.x);
+  const int64_t block = static_cast<int64_t>(blockIdx.y) * kJoinRow + blockIdx.x, task = WAVES == 1 ? block * kWaves + wave : block;
   const int row = static_cast<int>(task / a.q_heads), head = static_cast<int>(task % a.q_heads);
   if (row >= a.M) return;
   int seq = row;
@@ -943,9 +946,12 @@ template <int D, int BITS> static int run(const AttendArgs& a, const AttendPlan&
   else if (n.row_tiles == 0) attend_rows_kernel<D, BITS, 4><<<grid, block, 0, st>>>(a, n, p.parts);
   else if (n.row_tiles == 1) attend_tile_kernel<D, BITS, 1><<<grid, block, 0, st>>>(a, n, p.parts);
   else attend_tile_kernel<D, BITS, 2><<<grid, block, 0, st>>>(a, n, p.parts);
-  const int64_t outputs = static_cast<int64_t>(a.M) * a.q_heads;
-  if (p.parts > 16) attend_join_kernel<D, 4><<<static_cast<unsigned>(outputs), 64 * kWaves, 0, st>>>(a, p);
-  else if (p.parts > 1) attend_join_kernel<D, 1><<<static_cast<unsigned>(ceil_div(outputs, kWaves)), 64 * kWaves, 0, st>>>(a, p);
+  if (p.parts > 1) {
+    const int64_t outputs = static_cast<int64_t>(a.M) * a.q_heads, blocks = p.parts > 16 ? outputs : ceil_div(outputs, kWaves);
+    const dim3 join(static_cast<unsigned>(std::min<int64_t>(blocks, kJoinRow)), static_cast<unsigned>(ceil_div(blocks, kJoinRow)));
+    if (p.parts > 16) attend_join_kernel<D, 4><<<join, block, 0, st>>>(a, p);
+    else attend_join_kernel<D, 1><<<join, block, 0, st>>>(a, p);
+  }
   const hipError_t e = hipGetLastError();
   if (e == hipSuccess) return ROSAQ_OK;
   try { set_error(std::string("attention: ") + hipGetErrorString(e)); } catch (...) {}     // no memory for the text
