@@ -117,7 +117,8 @@ def rope_table(positions: int, rot_dim: int, base: float = 10000.0, scaling: int
 
 
 def rope(r: Rope, x: torch.Tensor, positions: torch.Tensor, head_dim: int, out: torch.Tensor | None = None) -> torch.Tensor:
-    """x with its heads turned to their rows' positions (int32 [M]); out may be x."""
+    """x with its heads turned to their rows' positions (int32 [M]); out may be x.  Rows whose position lies outside the table stay as
+    they are in out, and are zero without it."""
     M, width = x.shape
     ldx = _ld("x", x, M, width)
     if width % head_dim:
@@ -127,7 +128,7 @@ def rope(r: Rope, x: torch.Tensor, positions: torch.Tensor, head_dim: int, out: 
     if device != _current_device():
         with torch.cuda.device(device):
             return rope(r, x, positions, head_dim, out)
-    y = torch.empty((M, width), dtype=_HALF, device=x.device) if out is None else out
+    y = torch.zeros((M, width), dtype=_HALF, device=x.device) if out is None else out
     B.rosaq_rope(r.args, at, x.data_ptr(), M, ldx, width // head_dim, head_dim, y.data_ptr(), _ld("out", y, M, width), _stream_on(device))
     return y
 
@@ -145,7 +146,8 @@ class KvCache:
 def cache_append(cache: KvCache, slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, rope: Rope | None = None,
                  positions: torch.Tensor | None = None, q: torch.Tensor | None = None, q_out: torch.Tensor | None = None):
     """rosaq_cache_append: keys and values of M tokens to their slots (int64 [M]), keys turned first where `rope` is given, and
-    the queries q beside them.  Returns the turned queries (None without q); q_out may be q."""
+    the queries q beside them.  Returns the turned queries (None without q); q_out may be q.  Rows of skipped tokens stay as they are
+    in q_out, and are zero without it."""
     M = k.size(0)
     ldk, ldv = _ld("k", k, M, cache.width), _ld("v", v, M, cache.width)
     at_slots = _integers("slots", slots, _INT64, M)
@@ -168,14 +170,15 @@ def cache_append(cache: KvCache, slots: torch.Tensor, k: torch.Tensor, v: torch.
     ldq = _ld("q", q, M, width)
     if width % cache.head_dim:
         raise ValueError("q must hold whole heads")
-    y = torch.empty((M, width), dtype=_HALF, device=q.device) if q_out is None else q_out
+    y = torch.zeros((M, width), dtype=_HALF, device=q.device) if q_out is None else q_out
     B.rosaq_cache_append(cache.args, at_slots, M, k.data_ptr(), ldk, v.data_ptr(), ldv, angles, at, q.data_ptr(), ldq,
                          width // cache.head_dim, y.data_ptr(), _ld("q_out", y, M, width), _stream_on(device))
     return y
 
 
 def cache_read(cache: KvCache, slots: torch.Tensor, k: torch.Tensor | None = None, v: torch.Tensor | None = None):
-    """rosaq_cache_read: (k, v), the values of the slots; both are allocated where neither is given, one alone is read alone."""
+    """rosaq_cache_read: (k, v), the values of the slots; both are allocated where neither is given, one alone is read alone.  Rows of
+    slots that are none of the cache's stay as they are in what is given, and are zero in what is allocated."""
     M = slots.numel()
     at = _integers("slots", slots, _INT64, M)
     device = _device_of(slots, cache.data, k, v)
@@ -183,7 +186,7 @@ def cache_read(cache: KvCache, slots: torch.Tensor, k: torch.Tensor | None = Non
         with torch.cuda.device(device):
             return cache_read(cache, slots, k, v)
     if k is None and v is None:
-        k, v = (torch.empty((M, cache.width), dtype=_HALF, device=slots.device) for _ in range(2))
+        k, v = (torch.zeros((M, cache.width), dtype=_HALF, device=slots.device) for _ in range(2))
     pk, ldk = (0, 0) if k is None else (k.data_ptr(), _ld("k", k, M, cache.width))
     pv, ldv = (0, 0) if v is None else (v.data_ptr(), _ld("v", v, M, cache.width))
     B.rosaq_cache_read(cache.args, at, M, pk, ldk, pv, ldv, _stream_on(device))

@@ -34,3 +34,53 @@ def test_joins_of_very_many_outputs(parts, M, kv, tokens):
     assert bool((y[-2] == 9.0).all())
     del plan, q, y
     torch.cuda.empty_cache()
+
+
+# ---- results that the calls allocate -------------------------------------------------------------
+
+def _stale(rows, width):
+    """Leaves NaN where the allocator will put the next matrix of this shape."""
+    t = torch.full((rows, width), float("nan"), dtype=torch.float16, device="cuda")
+    at = t.data_ptr()
+    del t
+    return at
+
+
+def test_rows_without_a_position_or_slot_are_zero_where_the_call_allocates():
+    print("case allocated results", flush=True)
+    rng = np.random.default_rng(0)
+    x = rng.standard_normal((33, 256)).astype(np.float16)
+    at = np.arange(33, dtype=np.int32)
+    at[[4, 32]] = -1
+    ang = A.rope_angles(33, 128)
+    table = np.stack([np.cos(ang), np.sin(ang)], -1).astype(np.float32)
+    want = A.rope(x, table[at, :, 0], table[at, :, 1], 128, "half")
+    want[[4, 32]] = 0
+    r = T.Rope(dev(table))
+    cache = T.KvCache(2, 128, 8, 16, 3)
+    slots = np.arange(33, dtype=np.int64)
+    slots[7] = -1
+    xd, ad, sd = dev(x), dev(at), dev(slots)
+
+    where = _stale(33, 256)
+    y = T.rope(r, xd, ad, 128)
+    assert y.data_ptr() == where
+    same_bits(y, want)
+    del y
+
+    where = _stale(33, 256)
+    y = T.cache_append(cache, sd, xd, xd, rope=r, positions=ad, q=xd)
+    assert y.data_ptr() == where
+    skipped = want.copy()
+    skipped[7] = 0
+    same_bits(y, skipped)
+    del y
+
+    T.cache_append(cache, sd, xd, xd)
+    del xd
+    _stale(33, 256)
+    k, v = T.cache_read(cache, sd)
+    held = A.held(x, 2, 8).astype(np.float16).reshape(33, 256)
+    held[7] = 0
+    same_bits(k, held)
+    same_bits(v, held)
