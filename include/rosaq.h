@@ -369,7 +369,8 @@ typedef struct {
                                     /* NULL: sequence b has row b (max_rows 1)                          */
   const int32_t* kv_len_dev;        /* DEVICE int32 [sequences]                                         */
   const int32_t* pages_dev;         /* DEVICE int32 [sequences x page_stride]: pages of a sequence's tokens, in order.  Tokens of a */
-  int32_t page_stride;              /* page outside [0, num_pages) are seen by no row; lengths are cut to page_stride pages */
+  int32_t page_stride;              /* page outside [0, num_pages) are seen by no row; lengths are cut to page_stride pages (0: */
+                                    /* no tokens, pages_dev may be NULL)                                */
   const int32_t* prefix_pages_dev;  /* DEVICE int32 [ceil(prefix_len / page_tokens)], NULL without a prefix */
 } rosaq_attention_desc;
 

@@ -142,9 +142,10 @@ static int check_attention(const rosaq_attention_desc* d, AttendArgs* a, bool po
     if ((rc = check_matrix("y", d->y_dev, d->ldy, width)) != ROSAQ_OK) return rc;
     if (overlap(d->q_dev, d->ldq, width, d->y_dev, d->ldy, width, d->M)) return fail(ROSAQ_ERR_ARG, "y must not overlap q");
     if (!d->kv_len_dev) return fail(ROSAQ_ERR_NULL, "kv_len_dev is NULL");
-    if (d->max_kv > 0 && !d->pages_dev) return fail(ROSAQ_ERR_NULL, "pages_dev is NULL");
-    if (d->prefix_len > 0 && !d->prefix_pages_dev) return fail(ROSAQ_ERR_NULL, "prefix_pages_dev is NULL");
     if (d->page_stride < 0) return fail(ROSAQ_ERR_SHAPE, "page_stride must not be negative");
+    // a table of no columns has no address: no sequence has tokens then
+    if (d->max_kv > 0 && d->page_stride > 0 && !d->pages_dev) return fail(ROSAQ_ERR_NULL, "pages_dev is NULL");
+    if (d->prefix_len > 0 && !d->prefix_pages_dev) return fail(ROSAQ_ERR_NULL, "prefix_pages_dev is NULL");
     if (misaligned(d->kv_len_dev, 4) || misaligned(d->row_start_dev, 4) || misaligned(d->pages_dev, 4) || misaligned(d->prefix_pages_dev, 4))
       return fail(ROSAQ_ERR_ALIGN, "the integer arrays must be 4-byte aligned");
   }

@@ -84,3 +84,17 @@ def test_rows_without_a_position_or_slot_are_zero_where_the_call_allocates():
     held[7] = 0
     same_bits(k, held)
     same_bits(v, held)
+
+
+# ---- tables without a column ---------------------------------------------------------------------
+
+def test_page_table_cut_to_no_column():
+    """No sequence has tokens of its own yet: the table, cut to the pages in use, has no column."""
+    print("case no column", flush=True)
+    b = Batch(3, [0, 0, 0], [1, 1, 1], 2, 2, 64, 4, 32, prefix=70)
+    b.append()
+    plan = b.plan(max_kv=500)
+    y = torch.full((3, 256), 9.0, dtype=torch.float16, device="cuda")
+    T.attention(plan, dev(b.q), dev(np.array([0, 9, 0], np.int32)), torch.empty((3, 0), dtype=torch.int32, device="cuda"),
+                prefix_pages=dev(b.prefix_table), out=y)
+    b.check(y)
