@@ -349,7 +349,8 @@ int rosaq_cache_read(const rosaq_cache* cache, const int64_t* slots_dev, int32_t
 /* rosaq_attention - y = softmax(scale q K^T) V for the rows of several sequences over their tokens in the cache:
  * from one new token a sequence to whole prompts, with or without a prefix that all sequences share.
  * Row i of a sequence of n rows and l cached tokens (the rows' own tokens among them, appended before) sees all of the prefix
- * and, of the sequence's tokens, all (causal 0) or those below l - n + i + 1 (causal 1).  A row that sees nothing is zero.
+ * and, of the sequence's tokens, all (causal 0) or those below l - n + i + 1 (causal 1).  A row that sees nothing is zero; one that
+ * sees tokens with a query head that holds NaN or Inf, or sees a token whose keys or values of its kv head read as NaN, is NaN there.
  * q_heads is a multiple of the cache's kv_heads: query head h reads kv head h / (q_heads / kv_heads).
  * Scores, sums and the softmax's statistics are fp32; a probability times the scale of its token's values is rounded to fp16 once for the
  * product with their codes, and y once. */

@@ -159,6 +159,13 @@ template <int D> struct Part {
       : sums(a.part), stats(reinterpret_cast<float2*>(a.part + static_cast<int64_t>(parts) * a.M * a.q_heads * D)) {}
 };
 
+// Eight channels of a query, infinities as NaN (inf * 0 + inf).  A channel that is no number makes every score of its row one: infinite in one
+// sign or both, or NaN, and the softmax of each is NaN.  Scores of -inf alone would look like a row that sees nothing, which is zero.
+__device__ __forceinline__ half8 load_query(const _Float16* p) {
+  const half8 h = as_h8(*reinterpret_cast<const uint4*>(p)), zero = {0, 0, 0, 0, 0, 0, 0, 0};
+  return __builtin_elementwise_fma(h, zero, h);
+}
+
 // The power of two above a scale | zero's scale: s < 2^exponent_of <= 2 s.  (Of 0 -14, of NaN 17.)
 __device__ __forceinline__ float exponent_of(uint32_t sz) { return static_cast<float>(static_cast<int>(sz >> 10 & 0x1fu) - 14); }
 
@@ -276,7 +283,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const AttendLau
                           (kv_head * a.group + my % a.group) * D + g * (D / 4);
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-      const half8 h = as_h8(reinterpret_cast<const uint4*>(src)[s]);
+      const half8 h = load_query(src + 8 * s);
       q[s] = BITS == 4 ? half8{h[0], h[4], h[1], h[5], h[2], h[6], h[3], h[7]} : h;
     }
   }
@@ -507,7 +514,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
                           (w.kv_head * a.group + my % a.group) * D + g * (D / 4);
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-      const half8 h = as_h8(reinterpret_cast<const uint4*>(src)[s]);
+      const half8 h = load_query(src + 8 * s);
       q[t][s] = BITS == 4 ? half8{h[0], h[4], h[1], h[5], h[2], h[6], h[3], h[7]} : h;
     }
   }

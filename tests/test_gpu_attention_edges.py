@@ -98,3 +98,26 @@ def test_page_table_cut_to_no_column():
     T.attention(plan, dev(b.q), dev(np.array([0, 9, 0], np.int32)), torch.empty((3, 0), dtype=torch.int32, device="cuda"),
                 prefix_pages=dev(b.prefix_table), out=y)
     b.check(y)
+
+
+# ---- queries that are no numbers -----------------------------------------------------------------
+
+@pytest.mark.parametrize("bits,dim", [(4, 64), (4, 128), (8, 64), (8, 128)])
+@pytest.mark.parametrize("rows", [1, 3, 20, 140])
+@pytest.mark.parametrize("odd", [-np.inf, np.inf, np.nan])
+def test_queries_that_are_no_numbers(bits, dim, rows, odd):
+    """A score of -inf alone leaves nothing to divide by: the row is NaN, not zero.  Its neighbours and rows that see nothing are as ever."""
+    print(f"case odd queries int{bits} {dim} rows {rows} {odd}", flush=True)
+    b = Batch(4, [rows, rows + 70, 0], [rows, rows, rows], 1, 2, dim, bits, 16)
+    b.k[:, 5] = np.abs(b.k[:, 5]) + 1          # one sign: every score has the same
+    b.append()
+    hit = [(0, 1), (rows - 1, 0), (rows, 1), (3 * rows - 1, 0)]
+    q = b.q.reshape(b.M, 2, dim).copy()
+    for row, head in hit:
+        q[row, head, 5] = odd
+    y = b.run(q=dev(q.reshape(b.M, -1))).cpu().numpy().astype(np.float64).reshape(b.M, 2, dim)
+    want, bound = b.oracle()
+    for row, head in hit[:3]:
+        assert np.isnan(y[row, head]).all(), (row, head)
+        y[row, head] = want[row, head]
+    assert np.all(np.abs(y - want) <= bound) and not y[2 * rows:].any()
