@@ -353,7 +353,8 @@ int rosaq_cache_read(const rosaq_cache* cache, const int64_t* slots_dev, int32_t
  * sees tokens with a query head that holds NaN or Inf, or sees a token whose keys or values of its kv head read as NaN, is NaN there.
  * q_heads is a multiple of the cache's kv_heads: query head h reads kv head h / (q_heads / kv_heads).
  * Scores, sums and the softmax's statistics are fp32; a probability times the scale of its token's values is rounded to fp16 once for the
- * product with their codes, and y once. */
+ * product with their codes, and y once.  Probabilities that are tiny next to the largest lose bits of the first of these, so that l tokens
+ * cost up to l 2^-34 of the largest value besides: 2^-14 of it at a million. */
 typedef struct {
   const rosaq_cache* cache;
   int32_t q_heads;

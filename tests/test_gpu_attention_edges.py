@@ -121,3 +121,39 @@ def test_queries_that_are_no_numbers(bits, dim, rows, odd):
         assert np.isnan(y[row, head]).all(), (row, head)
         y[row, head] = want[row, head]
     assert np.all(np.abs(y - want) <= bound) and not y[2 * rows:].any()
+
+
+# ---- many tokens of little weight ----------------------------------------------------------------
+
+@pytest.mark.parametrize("rows,seqs", [(1, 1040), (20, 512), (70, 512)])
+def test_many_tokens_of_little_weight(rows, seqs):
+    """Two million tokens of weight 2^-31 each beside one of 1: a thousandth of the answer, which the sum of the products must not
+    lose where the sum of the weights has it.  One part, so that all tokens of a row share a reference.  What a weight may lose is half a
+    step of fp16's subnormals, 2^-25, next to a largest of 2^10 at least, twice that against the largest value (the scale of a token is half its
+    largest value over the codes' at most)."""
+    n = 1 << 21
+    print(f"case {n} tokens of little weight, {rows} rows", flush=True)
+    cache = T.KvCache(1, 64, 4, 4096, n // 4096)
+    slots = torch.arange(n, device="cuda")
+    k, v = (torch.zeros((n, 64), dtype=torch.float16, device="cuda") for _ in range(2))
+    k[0, 0] = 1.0
+    v[0, 1] = 1.0
+    v[1:, 2] = 1.0
+    T.cache_append(cache, slots, k, v)
+    del k, v
+    M = seqs * rows
+    q = torch.zeros((M, 64), dtype=torch.float16, device="cuda")
+    q[:, 0] = 21.484375
+    plan = T.AttentionPlan(cache, 1, seqs, max_kv=n, max_rows=rows, rows=M, causal=False, scale=1.0)
+    assert plan.ws_bytes == 256                                     # one part
+    pages = torch.arange(n // 4096, dtype=torch.int32, device="cuda").repeat(seqs, 1)
+    y = T.attention(plan, q, torch.full((seqs,), n, dtype=torch.int32, device="cuda"), pages,
+                    row_start=torch.arange(seqs + 1, dtype=torch.int32, device="cuda") * rows).cpu().numpy().astype(np.float64)
+    one = 15 * float(np.float16(1 / 15))
+    w = np.exp(-21.484375 * one)
+    total = 1 + (n - 1) * w
+    assert 1e-3 > (total - 1) > 9e-4
+    want = np.zeros(64)
+    want[1], want[2] = one / total, (n - 1) * w * one / total
+    # the fp32 sums of the weights: 2^21 terms over four lanes' registers and waves, each sum off by half a step of what it has
+    assert np.all(np.abs(y - want) <= n * 2.0 ** -34 + 2.0 ** -11 * np.abs(want) + 2.0 ** -25)
