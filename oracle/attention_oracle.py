@@ -71,18 +71,26 @@ def held(x: np.ndarray, heads: int, bits: int) -> np.ndarray:
 
 def attention(q, k, v, limits, scale):
     """One sequence.  q fp16 [n, q_heads, d], k and v fp64 [tokens, kv_heads, d], limits [n]: row i sees tokens < limits[i]
-    (a boolean [n, tokens] serves too).  Returns (y fp64, bound): `bound` is how far an fp16 result may be off, from
-      w   the probabilities, a the score's sum of absolute products, e = 2^-11 half a step of fp16
-      probabilities rounded toward zero to fp16 in numerator and denominator alike:      2 e sum w |v - y|
-      values rounded to fp16:                                                            e sum w |v|
-      scores off by d = e a + (D + 8) 2^-24 a + 2^-20 (keys rounded to fp16; fp32 sums; scale and exponential),
-      in numerator and denominator:                                                      2 sum w d |v - y|
-      probabilities below fp16's normal range next to the largest, 2^5 at least:          tokens 2^-29 max |v|
-      the result's own rounding:                                                          e |y| + 2^-25"""
+    (a boolean [n, tokens] serves too).  Returns (y fp64, bound): `bound` is how far an fp16 result may be off if keys and values are
+    taken as they are, scores and sums are fp32, and a probability times its value's scale is rounded to fp16 once, to nearest, for
+    the product with the codes and not for the sum of the probabilities.  With
+      w   the probabilities, a the score's sum of absolute products, e = 2^-11 half a step of fp16, u = 2^-23 a whole step of fp32
+          (half of one if every addition rounds to nearest, which nothing says of those within a matrix instruction),
+    it adds up, to first order in e and u,
+      probabilities rounded for the product:            e sum w |v|
+      scores off by D = u ((d / 32 + 36) (a + 10) + 4 max a + 64): sums of d / 32 instructions that add 32 products in any order and may start from
+      a value's log2 s over the key's scale (|log2 s| <= 14, 10 in units of a natural logarithm); the scale's factors and the subtraction of the
+      reference; logarithm, reciprocal and exponential.  In numerator and denominator alike:
+                                                        sum w (exp D - 1) |v - y| / sum w exp(-D)
+      the sums over n tokens: products as above, weights of a lane one after the other, and up to 16 steps each that bring
+      parts and references together:                    u (n / 32 + 52) sum w |v| + u (n / 4 + 16) |y|
+      probabilities among fp16's subnormals, next to a largest of 2^10 at least, whose token's largest value is half its scale
+      times the codes' range at least, or whose scale is 2^-14:   n 2^-34 max(max |v|, 2^-7)
+      the result's own rounding:                        e |y| + 2^-25"""
     n, heads, d = q.shape
     group = heads // k.shape[1]
     tokens = k.shape[0]
-    e = 2.0 ** -11
+    e, u = 2.0 ** -11, 2.0 ** -23
     y = np.zeros((n, heads, d))
     bound = np.full((n, heads, d), 2.0 ** -25)
     for i in range(n):
@@ -97,8 +105,10 @@ def attention(q, k, v, limits, scale):
             w = np.exp(score - score.max())
             w /= w.sum()
             y[i, h] = w @ vv
-            off = np.abs(vv - y[i, h])
-            delta = (e + (d + 8) * 2.0 ** -24) * a + 2.0 ** -20
-            bound[i, h] += 2 * e * (w @ off) + e * (w @ np.abs(vv)) + 2 * ((w * delta) @ off)
-            bound[i, h] += tokens * 2.0 ** -29 * np.abs(vv).max() + e * np.abs(y[i, h])
+            off, size, out = np.abs(vv - y[i, h]), w @ np.abs(vv), np.abs(y[i, h])
+            delta = np.minimum(u * ((d / 32 + 36) * (a + 10) + 4 * a.max() + 64), 100.0)
+            b = e * size + (w * np.expm1(delta)) @ off / (w @ np.exp(-delta))
+            b += u * ((tokens / 32 + 52) * size + (tokens / 4 + 16) * out)
+            b += tokens * 2.0 ** -34 * max(np.abs(vv).max(), 2.0 ** -7)
+            bound[i, h] += b + e * (out + b)
     return y, bound
