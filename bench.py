@@ -26,6 +26,7 @@ before the timed region; dense rotations are seeded random orthogonal matrices.
 from __future__ import annotations
 
 import argparse
+import functools
 import json
 import os
 import sys
@@ -230,6 +231,25 @@ def shape_sweep(torch, shapes, ms_override, reps, emit):
         del W16, w16
 
 
+def decode_layer(B, T, lay, qkv, x, heads, xh, gated, y, ws, chained_mlp, attend=None):
+    """The linears of one layer on the current stream: q/k/v of x into the buffers of `qkv`, o of `heads`, the FFN of x.  `attend` is called
+    between q/k/v and o, to make `heads`; the rest is the same with and without it."""
+    M, sp = x.shape[0], T.current_stream_ptr()
+    B.rosaq_linear_batch(qkv, x.data_ptr(), M, x.stride(0), ws.data_ptr(), ws.numel(), sp)
+    if attend is not None:
+        attend()
+    T.linear(lay["o"], heads, y, ws)
+    if chained_mlp:
+        # gate and up in one launch, silu(gate) * up applied in its epilogue and written as the
+        # down projection's input fragments; then the down projection
+        B.rosaq_mlp_swiglu(lay["gate"], lay["up"], lay["down"], x.data_ptr(), M, x.stride(0), y.data_ptr(), y.stride(0),
+                           ws.data_ptr(), ws.numel(), sp)
+    else:
+        B.rosaq_linear_swiglu(lay["gate"], lay["up"], x.data_ptr(), M, x.stride(0), gated.data_ptr(), gated.stride(0),
+                              ws.data_ptr(), ws.numel(), sp)
+        T.linear(lay["down"], xh, y, ws)
+
+
 def decode_workload(torch, steps, warmup, absorbed=False, chained_mlp=True, context=0, cache_bits=4):
     """The linears of a LLaMA-7B-shaped decode step at batch 64, INT4 g128, K = 128: per layer
     q/k/v (one batched call, shared head-wise rotation), o (head-wise), gate/up (one batched call
@@ -278,29 +298,16 @@ def decode_workload(torch, steps, warmup, absorbed=False, chained_mlp=True, cont
            for lay in layers]
 
     def step():
-        sp = T.current_stream_ptr()
         for l, lay in enumerate(layers):
-            B.rosaq_linear_batch(qkv[l], x.data_ptr(), M, x.stride(0), ws.data_ptr(), ws.numel(), sp)
-            T.linear(lay["o"], x, y_d[3], ws)
-            if chained_mlp:
-                # gate and up in one launch, silu(gate) * up applied in its epilogue and written as the
-                # down projection's input fragments; then the down projection
-                B.rosaq_mlp_swiglu(lay["gate"], lay["up"], lay["down"], x.data_ptr(), M, x.stride(0),
-                                   y_d[3].data_ptr(), y_d[3].stride(0), ws.data_ptr(), ws.numel(), sp)
-            else:
-                B.rosaq_linear_swiglu(lay["gate"], lay["up"], x.data_ptr(), M, x.stride(0), y_f[0].data_ptr(),
-                                      y_f[0].stride(0), ws.data_ptr(), ws.numel(), sp)
-                T.linear(lay["down"], xh, y_d[3], ws)
+            decode_layer(B, T, lay, qkv[l], x, x, xh, y_f[0], y_d[3], ws, chained_mlp)
 
     def step_with_attention():
-        sp = T.current_stream_ptr()
-        for l, lay in enumerate(layers):
-            B.rosaq_linear_batch(qkv[l], x.data_ptr(), M, x.stride(0), ws.data_ptr(), ws.numel(), sp)
+        def attend(l):
             T.cache_append(caches[l], slots, y_d[1], y_d[2], rope=rope, positions=positions, q=y_d[0], q_out=y_d[0])
             T.attention(plans[l], y_d[0], lengths, pages, out=y_att)
-            T.linear(lay["o"], y_att, y_d[3], ws)
-            B.rosaq_mlp_swiglu(lay["gate"], lay["up"], lay["down"], x.data_ptr(), M, x.stride(0),
-                               y_d[3].data_ptr(), y_d[3].stride(0), ws.data_ptr(), ws.numel(), sp)
+
+        for l, lay in enumerate(layers):
+            decode_layer(B, T, lay, qkv[l], x, y_att, xh, y_f[0], y_d[3], ws, chained_mlp, functools.partial(attend, l))
 
     if context:
         page = 64
