@@ -171,6 +171,13 @@ __device__ __forceinline__ half8 load_query(const _Float16* p) {
 // The power of two above a scale | zero's scale: s < 2^exponent_of <= 2 s.  (Of 0 -14, of NaN 17.)
 __device__ __forceinline__ float exponent_of(uint32_t sz) { return static_cast<float>(static_cast<int>(sz >> 10 & 0x1fu) - 14); }
 
+// Two channels of a row's answer: means of values that fp16 holds, times what the probabilities' rounding makes of them, at most 1 + 2^-11.  Above 65520
+// that would be infinite, and stays at the largest number instead.  NaN passes (minimum and maximum keep it, unlike min and max).
+__device__ __forceinline__ half2v answer(float a, float b) {
+  const half2v most = {(_Float16)65504.f, (_Float16)65504.f};
+  return __builtin_elementwise_maximum(__builtin_elementwise_minimum(half2v{static_cast<_Float16>(a), static_cast<_Float16>(b)}, most), -most);
+}
+
 // A lane's share of a row, channels 4 g U .. + 4 U - 1, to y or to the row's partial results.
 template <int D>
 __device__ __forceinline__ void store_row(const AttendArgs& a, const Part<D>& out, int parts, int part, int64_t token, int head, int g,
@@ -181,9 +188,9 @@ __device__ __forceinline__ void store_row(const AttendArgs& a, const Part<D>& ou
     _Float16* y = static_cast<_Float16*>(a.y) + token * a.ldy + head * D + 4 * g * U;
 #pragma unroll
     for (int e = 0; e < 4 * U / 8; ++e) {
-      half8 h;
+      half2v h[4];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) h[i] = static_cast<_Float16>(sum[(8 * e + i) % U][(8 * e + i) / U] * inv);
+      for (int i = 0; i < 8; i += 2) h[i / 2] = answer(sum[(8 * e + i) % U][(8 * e + i) / U] * inv, sum[(8 * e + i + 1) % U][(8 * e + i + 1) / U] * inv);
       reinterpret_cast<uint4*>(y)[e] = __builtin_bit_cast(uint4, h);
     }
   } else {
@@ -424,7 +431,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const AttendLau
       if (parts == 1) {
         const float inv = total == 0.f ? 0.f : 1.f / total;
         *reinterpret_cast<half2v*>(static_cast<_Float16*>(a.y) + token * a.ldy + head * D + ch) =
-            half2v{static_cast<_Float16>(y0 * inv), static_cast<_Float16>(y1 * inv)};
+            answer(y0 * inv, y1 * inv);
       } else {
         const int64_t at = (static_cast<int64_t>(part) * a.M + token) * a.q_heads + head;
         *reinterpret_cast<float2*>(out.sums + at * D + ch) = make_float2(y0, y1);
@@ -879,7 +886,7 @@ __global__ __launch_bounds__(64 * kWaves) void attend_join_kernel(AttendArgs a, 
   _Float16* to = static_cast<_Float16*>(a.y) + row * a.ldy + head * D + ch;
 #pragma unroll
   for (int e = 0; e < C; e += 2)
-    *reinterpret_cast<half2v*>(to + e) = half2v{static_cast<_Float16>(y[e] * inv), static_cast<_Float16>(y[e + 1] * inv)};
+    *reinterpret_cast<half2v*>(to + e) = answer(y[e] * inv, y[e + 1] * inv);
 }
 
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }

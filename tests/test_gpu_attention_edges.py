@@ -157,3 +157,27 @@ def test_many_tokens_of_little_weight(rows, seqs):
     want[1], want[2] = one / total, (n - 1) * w * one / total
     # the fp32 sums of the weights: 2^21 terms over four lanes' registers and waves, each sum off by half a step of what it has
     assert np.all(np.abs(y - want) <= n * 2.0 ** -34 + 2.0 ** -11 * np.abs(want) + 2.0 ** -25)
+
+
+# ---- means of the largest numbers ----------------------------------------------------------------
+
+@pytest.mark.parametrize("tokens", [100, 600])
+@pytest.mark.parametrize("rows", [16, 40, 140])
+def test_means_of_the_largest_numbers(rows, tokens):
+    """Values of 178 x 368 = 65504 and its negative, which the cache holds exactly: their mean is finite, whatever the probabilities' rounding
+    adds up to (up to 2^-11, and from 2^-12 on the sum is nearer to 2^16).  Directly stored and joined."""
+    print(f"case largest numbers, {rows} rows, {tokens} tokens", flush=True)
+    seqs = 6
+    b = Batch(2, [tokens] * seqs, [rows] * seqs, 2, 1, 64, 8, 64, causal=False)
+    b.k[:] = 0
+    b.k[np.arange(len(b.k)) % tokens % 32 == 0, ::64] = 1.0       # one token of every 32, to which the others' weights are rounded
+    b.v[:] = 65504
+    b.v[:, 1] = -28336                              # scale 368, zero 77
+    b.v[:, 64:] = -b.v[:, :64]                      # zero 178
+    b.q[:] = 0
+    b.q[:, ::64] = np.linspace(0.05, 2.0, b.M)[:, None].astype(np.float16)
+    b.scale = 1.0
+    held = A.held(b.v, 2, 8)
+    assert held.max() == 65504 and held.min() == -65504
+    b.append()
+    b.check(b.run(b.plan(scale=1.0)))
