@@ -352,6 +352,7 @@ int rosaq_cache_read(const rosaq_cache* cache, const int64_t* slots_dev, int32_t
  * and, of the sequence's tokens, all (causal 0) or those below l - n + i + 1 (causal 1).  A row that sees nothing is zero; one that
  * sees tokens with a query head that holds NaN or Inf, or sees a token whose keys or values of its kv head read as NaN, is NaN there.
  * q_heads is a multiple of the cache's kv_heads: query head h reads kv head h / (q_heads / kv_heads).
+ * Every token below a sequence's length must have been appended: one that was not holds whatever the memory held.
  * Scores, sums and the softmax's statistics are fp32; a probability times the scale of its token's values is rounded to fp16 once for the
  * product with their codes, and y once.  Probabilities that are tiny next to the largest lose bits of the first of these, so that l tokens
  * cost up to l 2^-34 of the largest value besides: 2^-14 of it at a million. */
@@ -377,7 +378,10 @@ typedef struct {
 } rosaq_attention_desc;
 
 /* ws_dev: DEVICE scratch of rosaq_workspace_bytes_attention(desc) bytes, 256-byte aligned, needs no initialisation; the
- * size depends on the cache's shape and the numbers of the first block of the struct alone (pointers may still be NULL).  Calls that share
+ * size depends on the cache's shape and the numbers of the first block of the struct alone (pointers may still be NULL).  It does not grow with
+ * them throughout: calls of few sequences are split further, so that a smaller batch may need more (32 heads, max_kv 4096: 256 bytes for 64
+ * sequences, 1 MB for 32); a loop over several shapes takes the largest of their sizes.  How a call is split goes by max_kv, not by
+ * the lengths, which the host does not see: the nearer max_kv is to them, the better short sequences are spread.  Calls that share
  * a workspace must not overlap in time.  Errors: NULL, SHAPE, ARG, ALIGN, WORKSPACE, HIP (workspace_bytes: 0 on any). */
 size_t rosaq_workspace_bytes_attention(const rosaq_attention_desc* desc);
 int rosaq_attention(const rosaq_attention_desc* desc, void* ws_dev, size_t ws_bytes, void* hip_stream);

@@ -453,9 +453,9 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const AttendLau
 // which the product does not notice, but their weights would be missing here.
 //
 // Measured: four prompts of 2048 tokens x 32 heads (8 bits) 180 to 186 us = 740 to 766 TFLOP/s of the products that the mask leaves (a product of two
-// 8192 x 8192 fp16 matrices: 1133).  The matrix cores are busy 31 % of that; a stage of a wave takes 64 MFMAs of 16 cycles beside some 230 vector
-// operations (four cycles; sixteen for each of its 32 exponentials) and 32 KiB out of LDS, one stage after the other in each wave, and two waves a SIMD (240 registers) overlap
-// about half.  Built and slower: eight waves a workgroup with half of them half a stage behind (233 against 189 us: the barriers
+// 8192 x 8192 fp16 matrices: 1133).  A stage of a wave takes 62 MFMAs of 16 cycles and some 285 vector operations (four cycles, eight for each of its 32
+// exponentials), 31 % and 39 % of a SIMD's 442 thousand cycles.  One after the other they would take 70 %, so its two waves (240 registers) fill
+// none of each other's gaps on the whole: each waits for data or the barrier in 28 % of its cycles, and to issue in 28 %.  Built and slower: eight waves a workgroup with half of them half a stage behind (233 against 189 us: the barriers
 // cost more than the sharing saves), the factors of the next stage between the MFMAs by the scheduler's groups (spills; 260
 // against 239 on the 4-bit chunk), three and four row tiles a wave (spills), half a stage at a time and one stage's LDS for three workgroups
 // a unit (spills), priorities around either product (none or worse), the first codes before the queries (188 against 186).
@@ -896,9 +896,10 @@ static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // Kernel: up to 16 rows are one tile of attend_rows.  From 17 to 32 both are as fast (us, attend_tile / attend_rows: 8 sequences of up to 8192 tokens x 8
 // kv heads, 32 rows, 4 bits 41 / 38; 32 of up to 1024, 8 bits 28 / 29; one of 32768 27 / 30), at 48 rows attend_tile is (43 / 45, 33 / 48, 30 / 49).
 // Parts: enough workgroups for all compute units, eight steps or two stages in each at least.  More of them balance ragged lengths better and cost more
-// partial results: 16 sequences of 8192 to 32768 tokens in 1536 / 2048 / 2560 / 6144 workgroups 96 / 89 / 89 / 93 us; a chunk of 3 x 509 rows x 32 heads,
+// partial results: 16 sequences of 8192 to 32768 tokens in 1536 / 2048 / 6144 workgroups 96 / 89 / 93 us; a chunk of 3 x 509 rows x 32 heads,
 // 384 workgroups as they are 239 us, in 2, 3, 4 and 5 parts 292, 240, 286 and 224: which is best goes by the lengths, which the host does not
-// know.  A prefix under 64 rows, 32 heads: 256 / 512 workgroups 27.6 / 32.2 us beside the sequences' own.
+// know.  A prefix under 64 rows, 32 heads: 256 / 512 workgroups 27.6 / 32.2 us beside the sequences' own; under 384 rows, 8 heads, 16389 tokens:
+// 256 / 384 / 512 74.9 / 69.9 / 66.8.
 // Waves alone: where there are 2048 tiles of up to 16 steps (64 x 32 heads, us together / alone: 256 tokens 20.6 / 19.3, 512 34.2 / 32.3, 1024
 // 52.5 / 54.8).
 static AttendLaunch shape_launch(const AttendArgs& a, int over, int64_t rows, int64_t tokens_prefix, int64_t tokens_own, int64_t seqs) {

@@ -194,7 +194,8 @@ def cache_read(cache: KvCache, slots: torch.Tensor, k: torch.Tensor | None = Non
 
 
 class AttentionPlan:
-    """The bounds of attention calls over one cache and a workspace for them.  Calls with one plan must not overlap in time."""
+    """The bounds of attention calls over one cache and a workspace for them, of the size that these bounds need (fewer sequences may
+    need more).  Calls with one plan must not overlap in time."""
 
     def __init__(self, cache: KvCache, q_heads: int, sequences: int, max_kv: int, max_rows: int = 1, rows: int | None = None,
                  prefix_len: int = 0, causal: bool = True, scale: float | None = None):
