@@ -230,7 +230,7 @@ def attention(plan: AttentionPlan, q: torch.Tensor, kv_len: torch.Tensor, pages:
         at_prefix = _integers("prefix_pages", prefix_pages, _INT32, -1)
         if prefix_pages.numel() * plan.cache.page_tokens < plan.prefix_len:
             raise ValueError("prefix_pages hold fewer tokens than the prefix")
-    elif prefix_pages is not None:
+    elif prefix_pages is not None and prefix_pages.numel():
         raise ValueError("prefix_pages given, and the plan has no prefix")
     device = _device_of(q, kv_len, pages, plan.ws, row_start, prefix_pages, out)
     if device != _current_device():

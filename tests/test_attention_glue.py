@@ -27,6 +27,6 @@ def test_prefix_pages_and_the_plan_have_to_agree():
         _call(_plan(20))
     with pytest.raises(ValueError, match="fewer tokens"):
         _call(_plan(33), prefix_pages=pages)
-    for plan, kw in ((_plan(0), {}), (_plan(32), dict(prefix_pages=pages))):
+    for plan, kw in ((_plan(0), {}), (_plan(0), dict(prefix_pages=pages[:0])), (_plan(32), dict(prefix_pages=pages))):
         with pytest.raises(ValueError, match="lie on a GPU"):      # all else is right
             _call(plan, **kw)
