@@ -455,7 +455,8 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const AttendLau
 // Measured: four prompts of 2048 tokens x 32 heads (8 bits) 180 to 186 us = 740 to 766 TFLOP/s of the products that the mask leaves (a product of two
 // 8192 x 8192 fp16 matrices: 1133).  A stage of a wave takes 62 MFMAs of 16 cycles and some 285 vector operations (four cycles, eight for each of its 32
 // exponentials), 31 % and 39 % of a SIMD's 442 thousand cycles.  One after the other they would take 70 %, so its two waves (240 registers) fill
-// none of each other's gaps on the whole: each waits for data or the barrier in 28 % of its cycles, and to issue in 28 %.  Built and slower: eight waves a workgroup with half of them half a stage behind (233 against 189 us: the barriers
+// none of each other's gaps on the whole: each waits for data or the barrier in 28 % of its cycles, and to issue in 28 %.
+// Built and slower: eight waves a workgroup with half of them half a stage behind (233 against 189 us: the barriers
 // cost more than the sharing saves), the factors of the next stage between the MFMAs by the scheduler's groups (spills; 260
 // against 239 on the 4-bit chunk), three and four row tiles a wave (spills), half a stage at a time and one stage's LDS for three workgroups
 // a unit (spills), priorities around either product (none or worse), the first codes before the queries (188 against 186).
