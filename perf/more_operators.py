@@ -13,7 +13,8 @@ Kinds of case:
 
 What the operators compute:
   norm      h = x + residual in fp32, kept rounded to the residual's type; y = h / sqrt(mean(h^2) + eps) * weight from the unrounded h;
-            8 bits: scale = max |y| / 127, code = rne(y / scale), value code * scale
+            8 bits: scale = fp32(max |y| / 127), code = rne(y / scale), value code * scale, all before the value in 64 bits: a code next
+            to a border is as far off as its step when it falls to the other side
   window    row i of a sequence of n rows and l cached tokens is at p = l - n + i and sees token j <= p if j > p - window or j < sinks;
             y = softmax(q k^T / sqrt(dim)) v over them, zero where there are none; keys and values are what the cache's codes stand for:
             lo = min(0, min x), hi = max(0, max x), top = 2^bits - 1, s = fp16(max((hi - lo) / top, 2^-14)), z = rne(-lo / s) in [0, top],
@@ -228,15 +229,16 @@ def _quantise(x, heads, dim, bits):
 
 def _plain_norm(s):
     case = s["case"]
-    h = s["x"].float()
+    wide = torch.float64 if case["codes"] else torch.float32
+    h = s["x"].to(wide)
     out = []
     if case["residual"]:
-        h = h + s["residual"].float()
+        h = h + s["residual"].to(wide)
         out.append(h.to(TYPES[case["residual"]]))
-    y = h / torch.sqrt((h * h).mean(dim=-1, keepdim=True) + s["eps"]) * s["weight"].float()
+    y = h / torch.sqrt((h * h).mean(dim=-1, keepdim=True) + s["eps"]) * s["weight"].to(wide)
     if case["codes"]:
-        scale = y.abs().amax(dim=-1, keepdim=True) / 127.0
-        return out + [torch.round(y / scale) * scale, scale[:, 0]]
+        scale = (y.abs().amax(dim=-1, keepdim=True) / 127.0).float()
+        return out + [torch.round(y / scale.double()).float() * scale, scale[:, 0]]
     return out + [y.to(torch.float16)]
 
 
@@ -369,7 +371,7 @@ def _exact_norm(s, case):
     h *= torch.rsqrt(h.square().sum(1) / case["dim"] + s["eps"])[:, None]
     h *= s["weight"].double()
     if case["codes"]:
-        step = torch.maximum(h.max(1).values, -h.min(1).values) / 127
+        step = (torch.maximum(h.max(1).values, -h.min(1).values) / 127).float().double()
         return out + [torch.round(h / step[:, None]) * step[:, None], step]
     return out + [h]
 
