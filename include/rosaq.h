@@ -386,6 +386,40 @@ typedef struct {
 size_t rosaq_workspace_bytes_attention(const rosaq_attention_desc* desc);
 int rosaq_attention(const rosaq_attention_desc* desc, void* ws_dev, size_t ws_bytes, void* hip_stream);
 
+/* ---- around the projections: the norm in front of them, log probabilities behind the last -------------------
+ *
+ * Both take whole rows.  Asynchronous on hip_stream, allocate nothing, never synchronise, need no workspace and may be captured into a
+ * graph; the current device must be the one that holds the memory. */
+
+#define ROSAQ_F16  0
+#define ROSAQ_BF16 1
+#define ROSAQ_F32  2
+
+/* rosaq_rmsnorm - root-mean-square norm of rows, with the addition to the residual stream in front of it:
+ *     h = x + residual,  residual_out = h,  y = h / sqrt(mean(h^2) + eps) * weight
+ * h is an fp32 sum, rounded once more where the stream is fp16; y is made from h before that, in fp32 (the sum of squares of a row with an fp32
+ * residual in fp64), and rounded to fp16 once.  So a sum that fp16 does not hold is infinite in residual_out and right in y.
+ * Optionally (or instead of y) as codes of 8 bits, for a product that takes those:
+ *     scale = fp32(max |y| / 127),  code = rne(y / scale) in [-127, 127],  value code * scale
+ * from a y in fp64.  A row of zeros has scale 0; one with NaN, or an infinity, in y has scale NaN and codes 0.
+ * A row that holds an infinity is zero but there, where it is NaN; one of zeros with eps 0 is NaN. */
+typedef struct {
+  int32_t M, D;                      /* rows; channels: a multiple of 8 in [8, 32768]                    */
+  int32_t residual_type;             /* ROSAQ_F16 or ROSAQ_F32: of residual and residual_out             */
+  double eps;                        /* >= 0                                                             */
+  const void* x_dev; int64_t ldx;    /* DEVICE fp16 [M x D].  This matrix and all others: bases and rows 16-byte aligned (codes 8) */
+  const void* residual_dev; int64_t ld_residual;   /* DEVICE [M x D], or NULL: h = x                     */
+  void* residual_out_dev; int64_t ld_residual_out; /* DEVICE [M x D], or NULL: not wanted                */
+  const void* weight_dev;            /* DEVICE fp16 [D], 16-byte aligned, or NULL: ones                  */
+  void* y_dev; int64_t ldy;          /* DEVICE fp16 [M x D], or NULL: not wanted                         */
+  void* codes_dev; int64_t ld_codes; /* DEVICE int8 [M x D], or NULL: not wanted                         */
+  float* scales_dev;                 /* DEVICE [M], with codes                                           */
+} rosaq_rmsnorm_desc;
+
+/* y and residual_out may each be the matrix (base, ld and type) of x or of residual; outputs overlap nothing else.
+ * Errors: NULL, SHAPE, ARG (eps, type, overlap), ALIGN, HIP. */
+int rosaq_rmsnorm(const rosaq_rmsnorm_desc* desc, void* hip_stream);
+
 /* rosaq_stream_probe - measurement aid, no arithmetic of the method: one launch of
  * `workgroups` x `threads` in which every wave reads its own contiguous share of
  * src_dev (src_bytes in total, 1 KiB per load) and every workgroup then reads

@@ -14,6 +14,7 @@ import numpy as np
 
 Q_NONE, Q_FULL, Q_HEADWISE = 0, 1, 2
 ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+F16, BF16, F32 = 0, 1, 2
 ROPE_SCALE_NONE, ROPE_SCALE_LINEAR, ROPE_SCALE_WAVELENGTH = range(3)
 SELECT_TOP, SELECT_TOP_PER_HEAD, SELECT_BOTTOM, SELECT_CONSECUTIVE, SELECT_TOP_AND_BOTTOM = range(5)
 
@@ -27,7 +28,7 @@ EXPORTED = ["rosaq_pack_weights", "rosaq_workspace_bytes", "rosaq_workspace_byte
             "rosaq_linear_headwise_static", "rosaq_linear_batch", "rosaq_linear_swiglu", "rosaq_mlp_swiglu", "rosaq_workspace_bytes_mlp", "rosaq_stream_probe", "rosaq_packed_clone", "rosaq_pca_headwise", "rosaq_pca_full",
             "rosaq_packed_info", "rosaq_packed_export", "rosaq_tune", "rosaq_launch_shape", "rosaq_launch_many_rows", "rosaq_block_map", "rosaq_packed_image", "rosaq_free",
             "rosaq_cache_bytes", "rosaq_rope_table", "rosaq_rope", "rosaq_cache_append", "rosaq_cache_read", "rosaq_attention", "rosaq_workspace_bytes_attention",
-            "rosaq_last_error"]
+            "rosaq_rmsnorm", "rosaq_last_error"]
 
 
 class PackDesc(C.Structure):
@@ -60,6 +61,13 @@ class AttentionDesc(C.Structure):
                 ("scale", C.c_float), ("q", C.c_void_p), ("ldq", C.c_int64), ("y", C.c_void_p), ("ldy", C.c_int64),
                 ("row_start", C.c_void_p), ("kv_len", C.c_void_p), ("pages", C.c_void_p), ("page_stride", C.c_int32),
                 ("prefix_pages", C.c_void_p)]
+
+
+class RmsNormDesc(C.Structure):
+    _fields_ = [("M", C.c_int32), ("D", C.c_int32), ("residual_type", C.c_int32), ("eps", C.c_double), ("x", C.c_void_p), ("ldx", C.c_int64),
+                ("residual", C.c_void_p), ("ld_residual", C.c_int64), ("residual_out", C.c_void_p), ("ld_residual_out", C.c_int64),
+                ("weight", C.c_void_p), ("y", C.c_void_p), ("ldy", C.c_int64), ("codes", C.c_void_p), ("ld_codes", C.c_int64),
+                ("scales", C.c_void_p)]
 
 
 class RosaqError(RuntimeError):
@@ -143,6 +151,8 @@ def lib() -> C.CDLL:
         L.rosaq_workspace_bytes_attention.restype = sz
         L.rosaq_attention.argtypes = [C.POINTER(AttentionDesc), vp, sz, vp]
         L.rosaq_attention.restype = C.c_int
+        L.rosaq_rmsnorm.argtypes = [C.POINTER(RmsNormDesc), vp]
+        L.rosaq_rmsnorm.restype = C.c_int
         L.rosaq_free.argtypes = [vp]
         L.rosaq_free.restype = None
         L.rosaq_last_error.argtypes = []
@@ -341,6 +351,10 @@ def rosaq_workspace_bytes_attention(desc: AttentionDesc) -> int:
 
 def rosaq_attention(desc: AttentionDesc, ws_ptr: int, ws_bytes: int, stream: int = 0):
     _check(lib().rosaq_attention(desc, ws_ptr, ws_bytes, stream))
+
+
+def rosaq_rmsnorm(desc: RmsNormDesc, stream: int = 0):
+    _check(lib().rosaq_rmsnorm(desc, stream))
 
 
 def rosaq_stream_probe(src_ptr: int, src_bytes: int, shared_ptr: int, shared_bytes: int,

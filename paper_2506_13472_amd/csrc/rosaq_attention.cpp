@@ -5,21 +5,14 @@
 #include <string>
 
 #include "rosaq_attention.h"
-#include "rosaq_internal.h"
+#include "rosaq_checks.h"
 
 namespace rosaq {
-
-static int fail(int code, const char* msg) {
-  try { set_error(msg); } catch (...) {}
-  return code;
-}
 
 // Rows x heads: what the launches of rotary positions and cache, with 16 of them a workgroup of 256 threads, number in 32 bits.
 constexpr int64_t kMaxTasks = int64_t{1} << 27;
 constexpr int64_t kMaxGrid = int64_t{1} << 24;     // workgroups of 256 threads, of which a dimension of a grid has fewer than 2^32
 constexpr int kMaxSequences = 1 << 20;
-
-static bool misaligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n != 0; }
 
 static int check_heads(int32_t heads, int32_t head_dim) {
   if (head_dim != 64 && head_dim != 128) return fail(ROSAQ_ERR_ARG, "head_dim must be 64 or 128");
@@ -98,15 +91,9 @@ static int check_rope(const rosaq_rope_angles* r, const int32_t* positions, int3
   return ROSAQ_OK;
 }
 
-// Whether two matrices of M rows share elements.  With one leading dimension they may be columns of one buffer.
+// The same of fp16 matrices, in elements.
 static bool overlap(const void* x, int64_t ldx, int64_t wx, const void* y, int64_t ldy, int64_t wy, int M) {
-  const uintptr_t x0 = reinterpret_cast<uintptr_t>(x), x1 = x0 + 2 * (static_cast<uint64_t>(M - 1) * ldx + wx);
-  const uintptr_t y0 = reinterpret_cast<uintptr_t>(y), y1 = y0 + 2 * (static_cast<uint64_t>(M - 1) * ldy + wy);
-  if (!(x0 < y1 && y0 < x1)) return false;
-  if (ldx != ldy) return true;
-  const uint64_t row = 2 * static_cast<uint64_t>(ldx);
-  const uint64_t at = y0 >= x0 ? (y0 - x0) % row : (row - (x0 - y0) % row) % row;     // of y's rows within x's
-  return !(at >= 2 * static_cast<uint64_t>(wx) && at + 2 * static_cast<uint64_t>(wy) <= row);
+  return overlap_bytes(x, 2 * ldx, 2 * wx, y, 2 * ldy, 2 * wy, M);
 }
 static int check_in_place(const void* x, int64_t ldx, const void* y, int64_t ldy, int M, int64_t width) {
   if (x == y && ldx == ldy) return ROSAQ_OK;

@@ -1,0 +1,196 @@
+// Root-mean-square norm of rows, with the addition to the residual stream in front of it: h = x + residual, y = h / sqrt(mean h^2 + eps) * weight.
+//
+// A row is held by a team of threads, sixteen to 1024, in pieces of eight channels: read once, added up over the team, written once.  So it is bound
+// by memory, or by a launch where there are few rows.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <string>
+
+#include "rosaq_gemm.h"
+#include "rosaq_rows.h"
+
+namespace rosaq {
+
+// Eight channels of a row as they lie in memory; F32: those of the residual are fp32.
+template <bool F32> struct Residual { uint4 w; };
+template <> struct Residual<true> { float4 w[2]; };
+template <bool F32> __device__ __forceinline__ float channel(const Residual<F32>& r, int j) {
+  if constexpr (F32) return j < 4 ? (&r.w[0].x)[j] : (&r.w[1].x)[j - 4];
+  else return static_cast<float>(as_h8(r.w)[j]);
+}
+
+template <class T> __device__ __forceinline__ T add_(T a, T b) { return a + b; }
+// The larger; NaN where one is NaN.
+template <class T> __device__ __forceinline__ T larger(T a, T b) { return a != a ? a : (b != b ? b : (a > b ? a : b)); }
+
+// f over the values of a team's threads, in one order whatever runs when.
+template <int TEAM, class T, class F> __device__ __forceinline__ T reduce(T v, T* lds, F f) {
+#pragma unroll
+  for (int n = 1; n < (TEAM < 64 ? TEAM : 64); n *= 2) v = f(v, __shfl_xor(v, n, 64));
+  if constexpr (TEAM > 64) {
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x / 64] = v;
+    __syncthreads();
+    v = lds[0];
+#pragma unroll
+    for (int i = 1; i < TEAM / 64; ++i) v = f(v, lds[i]);
+  }
+  return v;
+}
+
+// ADD 0: no residual, 1: fp16, 2: fp32.  The sum of squares is fp32, of rows whose residual is fp32 in fp64: those may hold numbers whose squares
+// fp32 does not.  CODES: all in fp64, because a code next to a border is a whole step off when it falls to the other side; a step is a 127th of the largest
+// value.  The vector units have room for it (some 20 operations of 80 that fit beside a channel's way through memory).
+template <int TEAM, int CH, int ADD, bool CODES>
+__global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void rmsnorm_kernel(NormArgs a) {
+  constexpr int kThreads = TEAM < 256 ? 256 : TEAM, kTeams = kThreads / TEAM;
+  constexpr bool F32 = ADD == 2;
+  using Sum = std::conditional_t<F32 || CODES, double, float>;
+  using Value = std::conditional_t<CODES, double, float>;
+  __shared__ Sum lds_sum[TEAM > 64 ? TEAM / 64 : 1];
+  __shared__ Value lds_most[TEAM > 64 ? TEAM / 64 : 1];
+  const int t = threadIdx.x % TEAM, pieces = a.D / 8;
+  for (int64_t row = static_cast<int64_t>(blockIdx.x) * kTeams + threadIdx.x / TEAM; row < a.M; row += static_cast<int64_t>(gridDim.x) * kTeams) {
+    uint4 x[CH];
+    Residual<F32> r[CH];
+    uint4 w[CH];
+    const uint4* xs = reinterpret_cast<const uint4*>(static_cast<const _Float16*>(a.x) + row * a.ldx);
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      const int p = t + i * TEAM;
+      if (p >= pieces) continue;
+      x[i] = xs[p];
+      if constexpr (ADD == 1) r[i].w = reinterpret_cast<const uint4*>(static_cast<const _Float16*>(a.residual) + row * a.ld_residual)[p];
+      if constexpr (ADD == 2) {
+        const float4* rs = reinterpret_cast<const float4*>(static_cast<const float*>(a.residual) + row * a.ld_residual) + 2 * p;
+        r[i].w[0] = rs[0];
+        r[i].w[1] = rs[1];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      const int p = t + i * TEAM;
+      if (p >= pieces) continue;
+      if (a.weight) w[i] = static_cast<const uint4*>(a.weight)[p];
+    }
+    auto h = [&](int i, int j) {
+      const Value v = static_cast<Value>(static_cast<float>(as_h8(x[i])[j]));
+      if constexpr (ADD) return v + static_cast<Value>(channel<F32>(r[i], j));
+      else return v;
+    };
+    Sum sum = 0;
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+      if (t + i * TEAM < pieces)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const Sum v = static_cast<Sum>(h(i, j));
+          sum += v * v;
+        }
+    if constexpr (ADD != 0) {
+      if (a.residual_out) {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+          const int p = t + i * TEAM;
+          if (p >= pieces) continue;
+          if constexpr (F32) {
+            float4 o[2];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) (&o[j / 4].x)[j % 4] = static_cast<float>(h(i, j));
+            float4* to = reinterpret_cast<float4*>(static_cast<float*>(a.residual_out) + row * a.ld_residual_out) + 2 * p;
+            to[0] = o[0];
+            to[1] = o[1];
+          } else {
+            half8 o;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[j] = static_cast<_Float16>(static_cast<float>(h(i, j)));
+            reinterpret_cast<uint4*>(static_cast<_Float16*>(a.residual_out) + row * a.ld_residual_out)[p] = __builtin_bit_cast(uint4, o);
+          }
+        }
+      }
+    }
+    sum = reduce<TEAM>(sum, lds_sum, add_<Sum>);
+    Value factor;
+    if constexpr (std::is_same_v<Sum, double>) factor = static_cast<Value>(1.0 / sqrt(sum / a.D + a.eps));
+    else factor = 1.f / sqrtf(sum / static_cast<float>(a.D) + static_cast<float>(a.eps));
+    auto value = [&](int i, int j) {
+      const Value v = h(i, j) * factor;
+      return a.weight ? v * static_cast<Value>(static_cast<float>(as_h8(w[i])[j])) : v;
+    };
+    if (a.y) {
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        const int p = t + i * TEAM;
+        if (p >= pieces) continue;
+        half8 o;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[j] = static_cast<_Float16>(static_cast<float>(value(i, j)));
+        reinterpret_cast<uint4*>(static_cast<_Float16*>(a.y) + row * a.ldy)[p] = __builtin_bit_cast(uint4, o);
+      }
+    }
+    if constexpr (CODES) {
+      double most = 0.0;
+#pragma unroll
+      for (int i = 0; i < CH; ++i)
+        if (t + i * TEAM < pieces)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) most = larger(most, __builtin_fabs(value(i, j)));
+      most = reduce<TEAM>(most, lds_most, larger<double>);
+      const float scale = static_cast<float>(most / 127.0);
+      // a scale that is no positive number has no codes: zero's, or those of NaN
+      const double inverse = scale > 0.f && scale < INFINITY ? 1.0 / static_cast<double>(scale) : 0.0;
+      if (t == 0) a.scales[row] = scale < INFINITY ? scale : NAN;
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        const int p = t + i * TEAM;
+        if (p >= pieces) continue;
+        uint32_t o[2] = {0u, 0u};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          // a scale among fp32's subnormals is far from its 127th: codes are kept to their range
+          const int c = inverse == 0.0 ? 0 : min(max(static_cast<int>(__builtin_rint(value(i, j) * inverse)), -127), 127);
+          o[j / 4] |= (static_cast<uint32_t>(c) & 0xffu) << (j % 4 * 8);
+        }
+        reinterpret_cast<uint2*>(static_cast<char*>(a.codes) + row * a.ld_codes)[p] = make_uint2(o[0], o[1]);
+      }
+    }
+    if constexpr (TEAM > 64) __syncthreads();       // the next row's sums go to the same place
+  }
+}
+
+template <int TEAM, int CH, int ADD, bool CODES> static void run(const NormArgs& a, hipStream_t st) {
+  constexpr int kThreads = TEAM < 256 ? 256 : TEAM, kTeams = kThreads / TEAM;
+  const int64_t groups = (static_cast<int64_t>(a.M) + kTeams - 1) / kTeams;
+  rmsnorm_kernel<TEAM, CH, ADD, CODES><<<static_cast<unsigned>(std::min<int64_t>(groups, 1 << 20)), kThreads, 0, st>>>(a);
+}
+
+template <int TEAM, int CH> static void run(const NormArgs& a, hipStream_t st) {
+  const int add = !a.residual ? 0 : (a.residual_f32 ? 2 : 1);
+  if (a.codes) {
+    if (add == 0) run<TEAM, CH, 0, true>(a, st);
+    else if (add == 1) run<TEAM, CH, 1, true>(a, st);
+    else run<TEAM, CH, 2, true>(a, st);
+  } else {
+    if (add == 0) run<TEAM, CH, 0, false>(a, st);
+    else if (add == 1) run<TEAM, CH, 1, false>(a, st);
+    else run<TEAM, CH, 2, false>(a, st);
+  }
+}
+
+int launch_rmsnorm(const NormArgs& a, void* stream) {
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const int pieces = a.D / 8;
+  if (pieces <= 16) run<16, 1>(a, st);
+  else if (pieces <= 64) run<64, 1>(a, st);
+  else if (pieces <= 256) run<256, 1>(a, st);
+  else if (pieces <= 512) run<256, 2>(a, st);
+  else if (pieces <= 1024) run<256, 4>(a, st);
+  else if (pieces <= 2048) run<1024, 2>(a, st);
+  else run<1024, 4>(a, st);
+  const hipError_t e = hipGetLastError();
+  if (e == hipSuccess) return ROSAQ_OK;
+  try { set_error(std::string("rmsnorm: ") + hipGetErrorString(e)); } catch (...) {}     // no memory for the text
+  return ROSAQ_ERR_HIP;
+}
+
+}  // namespace rosaq

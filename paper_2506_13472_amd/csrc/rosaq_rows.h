@@ -1,0 +1,24 @@
+// What the kernels of whole rows are told: the norm in front of the projections, the log probabilities behind the last.
+#pragma once
+#include <cstdint>
+
+#include "rosaq.h"
+
+namespace rosaq {
+
+constexpr int kNormMaxWidth = 32768;
+
+struct NormArgs {
+  int M, D;
+  double eps;
+  const void* x; int64_t ldx;
+  const void* residual; int64_t ld_residual;      // null: none
+  void* residual_out; int64_t ld_residual_out;    // null: not wanted
+  int residual_f32;
+  const void* weight;                             // null: ones
+  void* y; int64_t ldy;                           // null: not wanted
+  void* codes; int64_t ld_codes; float* scales;   // null: not wanted
+};
+int launch_rmsnorm(const NormArgs& a, void* stream);
+
+}  // namespace rosaq

@@ -242,3 +242,69 @@ def attention(plan: AttentionPlan, q: torch.Tensor, kv_len: torch.Tensor, pages:
     d.kv_len, d.pages, d.page_stride, d.row_start, d.prefix_pages = at_len, at_pages, pages.size(1), at_rows, at_prefix
     B.rosaq_attention(d, plan.ws.data_ptr(), plan.ws_bytes, _stream_on(device))
     return y
+
+
+# ---- around the projections ------------------------------------------------------------------------------------------
+
+def _row_stride(name: str, x: torch.Tensor, rows: int, width: int, dtype: torch.dtype) -> int:
+    """As _ld, of any type."""
+    stride = x.stride()
+    if x.dtype is not dtype or x.shape != (rows, width) or stride[1] != 1:
+        raise ValueError(f"{name} must be a {dtype} tensor [{rows}, {width}] with unit column stride")
+    return stride[0] if rows > 1 else width
+
+
+def _rmsnorm(x, weight, eps, residual, residual_out, y, codes, scales):
+    """One rosaq_rmsnorm call on x's device; y, codes and scales: None, or where they go."""
+    M, D = x.shape
+    d = B.RmsNormDesc()
+    d.M, d.D, d.eps = M, D, eps
+    d.x, d.ldx = x.data_ptr(), _ld("x", x, M, D)
+    if weight is not None:
+        if weight.dtype is not _HALF or weight.shape != (D,) or not weight.is_contiguous():
+            raise ValueError(f"weight must be a contiguous fp16 tensor [{D}]")
+        d.weight = weight.data_ptr()
+    if residual is not None:
+        dtype = residual.dtype
+        if dtype is not _HALF and dtype is not torch.float32:
+            raise ValueError("residual must be fp16 or fp32")
+        d.residual_type = B.F16 if dtype is _HALF else B.F32
+        d.residual, d.ld_residual = residual.data_ptr(), _row_stride("residual", residual, M, D, dtype)
+        d.residual_out, d.ld_residual_out = residual_out.data_ptr(), _row_stride("residual_out", residual_out, M, D, dtype)
+    elif residual_out is not None:
+        raise ValueError("residual_out without a residual")
+    if y is not None:
+        d.y, d.ldy = y.data_ptr(), _ld("out", y, M, D)
+    if codes is not None:
+        d.codes, d.ld_codes = codes.data_ptr(), _row_stride("codes", codes, M, D, torch.int8)
+        if scales.dtype is not torch.float32 or scales.shape != (M,) or not scales.is_contiguous():
+            raise ValueError(f"scales must be a contiguous fp32 tensor [{M}]")
+        d.scales = scales.data_ptr()
+    device = _device_of(x, weight, residual, residual_out, y, codes, scales)
+    if device != _current_device():
+        with torch.cuda.device(device):
+            B.rosaq_rmsnorm(d, _stream_on(device))
+    else:
+        B.rosaq_rmsnorm(d, _stream_on(device))
+
+
+def rmsnorm(x: torch.Tensor, weight: torch.Tensor | None = None, eps: float = 1e-5, residual: torch.Tensor | None = None,
+            residual_out: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """rosaq_rmsnorm of x [M, D] + residual (fp16 or fp32): fp16 [M, D].  The sum goes to residual_out, which is residual itself
+    unless given; out may be x or residual where the sum does not go there."""
+    y = torch.empty(x.shape, dtype=_HALF, device=x.device) if out is None else out
+    _rmsnorm(x, weight, eps, residual, residual if residual_out is None else residual_out, y, None, None)
+    return y
+
+
+def rmsnorm_codes(x: torch.Tensor, weight: torch.Tensor | None = None, eps: float = 1e-5, residual: torch.Tensor | None = None,
+                  residual_out: torch.Tensor | None = None, codes: torch.Tensor | None = None, scales: torch.Tensor | None = None,
+                  out: torch.Tensor | None = None):
+    """rmsnorm in 8 bits: (codes int8 [M, D], scales fp32 [M]), a value being code * scale; in fp16 too where `out` is given."""
+    M, D = x.shape
+    if codes is None:
+        codes = torch.empty((M, D), dtype=torch.int8, device=x.device)
+    if scales is None:
+        scales = torch.empty(M, dtype=torch.float32, device=x.device)
+    _rmsnorm(x, weight, eps, residual, residual if residual_out is None else residual_out, out, codes, scales)
+    return codes, scales

@@ -1,0 +1,59 @@
+"""Argument checks of the norm and of the log probabilities, without a GPU."""
+import pytest
+
+from paper_2506_13472_amd import binding as B
+from test_attention_abi import ALIGN, ARG, NULL, SHAPE, W, X, Y, Z, _code
+
+
+def _norm(**over):
+    d = B.RmsNormDesc()
+    for k, v in dict(dict(M=4, D=512, residual_type=B.F16, eps=1e-5, x=X, ldx=512, residual=None, ld_residual=0, residual_out=None,
+                          ld_residual_out=0, weight=W, y=Y, ldy=512, codes=None, ld_codes=0, scales=None), **over).items():
+        setattr(d, k, v)
+    return B.rosaq_rmsnorm(d)
+
+
+def test_rmsnorm_refusals():
+    assert B.lib().rosaq_rmsnorm(None, None) == NULL
+    stream = dict(residual=Z, ld_residual=512)
+    kept = dict(stream, residual_out=Z + 0x400000, ld_residual_out=512)
+    codes = dict(codes=Z + 0x800000, ld_codes=512, scales=Z + 0xc00000)
+    assert _code(lambda: _norm(x=0)) == NULL and _code(lambda: _norm(y=0)) == NULL
+    assert _code(lambda: _norm(residual_out=Z, ld_residual_out=512)) == NULL               # no stream to keep
+    assert _code(lambda: _norm(**dict(codes, scales=0))) == NULL and _code(lambda: _norm(**dict(codes, codes=0))) == NULL
+    assert _code(lambda: _norm(M=0)) == SHAPE and _code(lambda: _norm(M=-3)) == SHAPE
+    for D in (0, -8, 4, 516, 32776, 65536):
+        assert _code(lambda: _norm(D=D, ldx=1 << 20, ldy=1 << 20)) == SHAPE, D
+    for eps in (-1e-9, float("nan"), float("inf")):
+        assert _code(lambda: _norm(eps=eps)) == ARG
+    for kind in (B.BF16, 3, -1):
+        assert _code(lambda: _norm(residual_type=kind)) == ARG
+    for name in ("ldx", "ldy"):
+        assert _code(lambda: _norm(**{name: 504})) == SHAPE and _code(lambda: _norm(**{name: 516})) == ALIGN
+        assert _code(lambda: _norm(**{name: (1 << 40) + 8})) == SHAPE
+    assert _code(lambda: _norm(x=X + 8)) == ALIGN and _code(lambda: _norm(y=Y + 2)) == ALIGN and _code(lambda: _norm(weight=W + 8)) == ALIGN
+    assert _code(lambda: _norm(**dict(stream, ld_residual=500))) == SHAPE
+    assert _code(lambda: _norm(**dict(stream, residual=Z + 4, residual_type=B.F32))) == ALIGN
+    assert _code(lambda: _norm(**dict(stream, ld_residual=514, residual_type=B.F32))) == ALIGN
+    assert _code(lambda: _norm(**dict(kept, ld_residual_out=0))) == SHAPE
+    assert _code(lambda: _norm(**dict(codes, codes=Z + 4))) == ALIGN and _code(lambda: _norm(**dict(codes, ld_codes=516))) == ALIGN
+    assert _code(lambda: _norm(**dict(codes, scales=Z + 2))) == ALIGN
+
+
+def test_rmsnorm_refuses_overlap():
+    stream = dict(residual=Z, ld_residual=512)
+    assert _code(lambda: _norm(y=X + 16)) == ARG and _code(lambda: _norm(y=X, ldy=1024)) == ARG         # not the same matrix
+    assert _code(lambda: _norm(y=X + 3 * 1024)) == ARG
+    assert _code(lambda: _norm(**stream, y=Z + 1024)) == ARG
+    assert _code(lambda: _norm(**stream, residual_out=Z + 16, ld_residual_out=512)) == ARG
+    assert _code(lambda: _norm(**stream, residual_out=Y, ld_residual_out=512)) == ARG                  # over y
+    assert _code(lambda: _norm(**stream, residual_out=Z, ld_residual_out=512, y=Z)) == ARG             # both in place
+    assert _code(lambda: _norm(**stream, residual_type=B.F32, y=Z)) == ARG                             # another type in its place
+    assert _code(lambda: _norm(**stream, residual_type=B.F32, residual_out=X, ld_residual_out=512)) == ARG
+    assert _code(lambda: _norm(weight=Y + 3 * 1024 + 512)) == ARG and _code(lambda: _norm(weight=Y)) == ARG
+    assert _code(lambda: _norm(codes=X, ld_codes=1024, scales=Z)) == ARG                               # codes lie nowhere in place
+    assert _code(lambda: _norm(codes=Z, ld_codes=512, scales=Z + 2044)) == ARG
+    assert _code(lambda: _norm(codes=Z, ld_codes=512, scales=Y + 4)) == ARG
+    # columns of one buffer are apart: the call gets to its next complaint
+    assert _code(lambda: _norm(ldx=2048, y=X + 1024, ldy=2048, weight=X + 2 * 512)) == ARG
+    assert _code(lambda: _norm(ldx=2048, y=X + 1008, ldy=2048)) == ARG and _code(lambda: _norm(ldx=2048, y=X + 2 * 1544, ldy=2048)) == ARG
