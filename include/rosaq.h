@@ -420,6 +420,30 @@ typedef struct {
  * Errors: NULL, SHAPE, ARG (eps, type, overlap), ALIGN, HIP. */
 int rosaq_rmsnorm(const rosaq_rmsnorm_desc* desc, void* hip_stream);
 
+/* rosaq_logprobs - of every row of logits x (what the head projection leaves), with a = scale (one over the temperature):
+ *     log p_v = a x_v - ln sum_w exp(a x_w),   entropy = - sum_v p_v log p_v   (p_v = 0 adds nothing)
+ * for the row's given tokens and for its `top` largest logits, largest first and of equal ones the lower index first.
+ * fp32; sums are taken from the row's largest logit on, so that large logits cost no accuracy.  A logit of -inf has p = 0: log p is -inf (as
+ * it is where it lies below fp32's range).  A row of -inf alone,
+ * and one that holds NaN or +inf, gets NaN for every log p and the entropy; its alternatives are still those of that order, NaN above all.
+ * A given token below zero is padding and gets 0, one of V or more gets NaN. */
+typedef struct {
+  int32_t M, V;                      /* rows; tokens of the vocabulary, at most 2^30                     */
+  int32_t type;                      /* ROSAQ_F16, _BF16 or _F32: of the logits                          */
+  float scale;                       /* 2^-60 to 2^60                                                    */
+  const void* logits_dev; int64_t ld;/* DEVICE [M x V], row m at logits + m * ld; any ld >= V, aligned to an element */
+  int32_t given;                     /* tokens given for every row, 0 to 4096                            */
+  int32_t top;                       /* alternatives, 0 to 64, at most V                                 */
+  const int64_t* tokens_dev;         /* DEVICE [M x given], NULL with given 0                            */
+  float* given_out_dev;              /* DEVICE [M x given], NULL with given 0                            */
+  float* entropy_dev;                /* DEVICE [M], or NULL: not wanted                                  */
+  int64_t* top_ids_dev;              /* DEVICE [M x top], NULL with top 0                                */
+  float* top_out_dev;                /* DEVICE [M x top], NULL with top 0                                */
+} rosaq_logprobs_desc;
+
+/* Outputs overlap nothing.  Errors: NULL, SHAPE, ARG (type, scale, overlap), ALIGN, HIP. */
+int rosaq_logprobs(const rosaq_logprobs_desc* desc, void* hip_stream);
+
 /* rosaq_stream_probe - measurement aid, no arithmetic of the method: one launch of
  * `workgroups` x `threads` in which every wave reads its own contiguous share of
  * src_dev (src_bytes in total, 1 KiB per load) and every workgroup then reads

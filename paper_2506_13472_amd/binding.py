@@ -28,7 +28,7 @@ EXPORTED = ["rosaq_pack_weights", "rosaq_workspace_bytes", "rosaq_workspace_byte
             "rosaq_linear_headwise_static", "rosaq_linear_batch", "rosaq_linear_swiglu", "rosaq_mlp_swiglu", "rosaq_workspace_bytes_mlp", "rosaq_stream_probe", "rosaq_packed_clone", "rosaq_pca_headwise", "rosaq_pca_full",
             "rosaq_packed_info", "rosaq_packed_export", "rosaq_tune", "rosaq_launch_shape", "rosaq_launch_many_rows", "rosaq_block_map", "rosaq_packed_image", "rosaq_free",
             "rosaq_cache_bytes", "rosaq_rope_table", "rosaq_rope", "rosaq_cache_append", "rosaq_cache_read", "rosaq_attention", "rosaq_workspace_bytes_attention",
-            "rosaq_rmsnorm", "rosaq_last_error"]
+            "rosaq_rmsnorm", "rosaq_logprobs", "rosaq_last_error"]
 
 
 class PackDesc(C.Structure):
@@ -68,6 +68,12 @@ class RmsNormDesc(C.Structure):
                 ("residual", C.c_void_p), ("ld_residual", C.c_int64), ("residual_out", C.c_void_p), ("ld_residual_out", C.c_int64),
                 ("weight", C.c_void_p), ("y", C.c_void_p), ("ldy", C.c_int64), ("codes", C.c_void_p), ("ld_codes", C.c_int64),
                 ("scales", C.c_void_p)]
+
+
+class LogprobsDesc(C.Structure):
+    _fields_ = [("M", C.c_int32), ("V", C.c_int32), ("type", C.c_int32), ("scale", C.c_float), ("logits", C.c_void_p), ("ld", C.c_int64),
+                ("given", C.c_int32), ("top", C.c_int32), ("tokens", C.c_void_p), ("given_out", C.c_void_p), ("entropy", C.c_void_p),
+                ("top_ids", C.c_void_p), ("top_out", C.c_void_p)]
 
 
 class RosaqError(RuntimeError):
@@ -153,6 +159,8 @@ def lib() -> C.CDLL:
         L.rosaq_attention.restype = C.c_int
         L.rosaq_rmsnorm.argtypes = [C.POINTER(RmsNormDesc), vp]
         L.rosaq_rmsnorm.restype = C.c_int
+        L.rosaq_logprobs.argtypes = [C.POINTER(LogprobsDesc), vp]
+        L.rosaq_logprobs.restype = C.c_int
         L.rosaq_free.argtypes = [vp]
         L.rosaq_free.restype = None
         L.rosaq_last_error.argtypes = []
@@ -355,6 +363,10 @@ def rosaq_attention(desc: AttentionDesc, ws_ptr: int, ws_bytes: int, stream: int
 
 def rosaq_rmsnorm(desc: RmsNormDesc, stream: int = 0):
     _check(lib().rosaq_rmsnorm(desc, stream))
+
+
+def rosaq_logprobs(desc: LogprobsDesc, stream: int = 0):
+    _check(lib().rosaq_logprobs(desc, stream))
 
 
 def rosaq_stream_probe(src_ptr: int, src_bytes: int, shared_ptr: int, shared_bytes: int,

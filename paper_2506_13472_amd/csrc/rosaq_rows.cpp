@@ -83,6 +83,43 @@ static int check_rmsnorm(const rosaq_rmsnorm_desc* d, NormArgs* a) {
   return ROSAQ_OK;
 }
 
+static int check_logprobs(const rosaq_logprobs_desc* d, LogprobArgs* a) {
+  if (!d) return fail(ROSAQ_ERR_NULL, "desc is NULL");
+  if (d->M < 1) return fail(ROSAQ_ERR_SHAPE, "M must be at least 1");
+  if (d->V < 1 || d->V > (1 << 30)) return fail(ROSAQ_ERR_SHAPE, "V must be in [1, 2^30]");
+  if (d->type != ROSAQ_F16 && d->type != ROSAQ_BF16 && d->type != ROSAQ_F32) return fail(ROSAQ_ERR_ARG, "type is not one of ROSAQ_F16, _BF16, _F32");
+  if (!(d->scale >= 0x1p-60f && d->scale <= 0x1p60f)) return fail(ROSAQ_ERR_ARG, "scale must be a number of 2^-60 to 2^60");
+  if (d->given < 0 || d->given > kMaxGiven) return fail(ROSAQ_ERR_SHAPE, "given must be in [0, 4096]");
+  if (d->top < 0 || d->top > kMaxTop || d->top > d->V) return fail(ROSAQ_ERR_SHAPE, "top must be in [0, 64] and at most V");
+  if (!d->given && !d->top && !d->entropy_dev) return fail(ROSAQ_ERR_NULL, "no output is wanted");
+  if (!d->logits_dev || (d->given && (!d->tokens_dev || !d->given_out_dev)) || (d->top && (!d->top_ids_dev || !d->top_out_dev)))
+    return fail(ROSAQ_ERR_NULL, "logits, or what `given` or `top` need, is NULL");
+  const int size = d->type == ROSAQ_F32 ? 4 : 2;
+  if (d->ld < d->V) return fail(ROSAQ_ERR_SHAPE, "logits: leading dimension smaller than width");
+  if (d->ld > (int64_t{1} << 40)) return fail(ROSAQ_ERR_SHAPE, "logits: leading dimension above 2^40");
+  if (misaligned(d->logits_dev, size) || misaligned(d->tokens_dev, 8) || misaligned(d->given_out_dev, 4) || misaligned(d->entropy_dev, 4) ||
+      misaligned(d->top_ids_dev, 8) || misaligned(d->top_out_dev, 4))
+    return fail(ROSAQ_ERR_ALIGN, "logits, tokens and outputs must be aligned to their elements");
+  const Matrix in[2] = {{"logits", d->logits_dev, d->ld * size, static_cast<int64_t>(d->V) * size},
+                        {"tokens", d->given ? d->tokens_dev : nullptr, 8 * d->given, 8 * d->given}};
+  const Matrix out[4] = {{"given_out", d->given ? d->given_out_dev : nullptr, 4 * d->given, 4 * d->given},
+                         {"entropy", d->entropy_dev, 4, 4},
+                         {"top_ids", d->top ? d->top_ids_dev : nullptr, 8 * d->top, 8 * d->top},
+                         {"top_out", d->top ? d->top_out_dev : nullptr, 4 * d->top, 4 * d->top}};
+  for (int o = 0; o < 4; ++o) {
+    if (!out[o].p) continue;
+    for (const Matrix& i : in)
+      if (i.p && overlap(out[o], i, d->M)) return overlapping(out[o], i);
+    for (int i = 0; i < o; ++i)
+      if (out[i].p && overlap(out[o], out[i], d->M)) return overlapping(out[o], out[i]);
+  }
+  a->M = d->M; a->V = d->V; a->type = d->type; a->logits = d->logits_dev; a->ld = d->ld; a->scale = d->scale;
+  a->given = d->given; a->tokens = d->tokens_dev; a->given_out = d->given_out_dev;
+  a->entropy = d->entropy_dev;
+  a->top = d->top; a->top_ids = d->top_ids_dev; a->top_out = d->top_out_dev;
+  return ROSAQ_OK;
+}
+
 }  // namespace rosaq
 
 using namespace rosaq;
@@ -93,6 +130,12 @@ int rosaq_rmsnorm(const rosaq_rmsnorm_desc* desc, void* hip_stream) {
   NormArgs a{};
   const int rc = check_rmsnorm(desc, &a);
   return rc != ROSAQ_OK ? rc : launch_rmsnorm(a, hip_stream);
+}
+
+int rosaq_logprobs(const rosaq_logprobs_desc* desc, void* hip_stream) {
+  LogprobArgs a{};
+  const int rc = check_logprobs(desc, &a);
+  return rc != ROSAQ_OK ? rc : launch_logprobs(a, hip_stream);
 }
 
 }  // extern "C"

@@ -21,4 +21,16 @@ struct NormArgs {
 };
 int launch_rmsnorm(const NormArgs& a, void* stream);
 
+constexpr int kMaxTop = 64, kMaxGiven = 4096;
+
+struct LogprobArgs {
+  int M, V, type;                                 // ROSAQ_F16, _BF16, _F32
+  const void* logits; int64_t ld;
+  float scale;
+  int given; const int64_t* tokens; float* given_out;
+  float* entropy;                                 // null: not wanted
+  int top; int64_t* top_ids; float* top_out;
+};
+int launch_logprobs(const LogprobArgs& a, void* stream);
+
 }  // namespace rosaq

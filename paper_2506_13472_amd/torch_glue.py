@@ -3,6 +3,7 @@ workspace, hand raw pointers and the current stream to the C ABI."""
 from __future__ import annotations
 
 import ctypes as C
+from typing import NamedTuple
 
 import torch
 
@@ -308,3 +309,60 @@ def rmsnorm_codes(x: torch.Tensor, weight: torch.Tensor | None = None, eps: floa
         scales = torch.empty(M, dtype=torch.float32, device=x.device)
     _rmsnorm(x, weight, eps, residual, residual if residual_out is None else residual_out, out, codes, scales)
     return codes, scales
+
+
+class LogProbs(NamedTuple):
+    """What logprobs returns; None where nothing was asked for."""
+
+    given: torch.Tensor | None        # fp32 [M, given]
+    entropy: torch.Tensor | None      # fp32 [M]
+    top_ids: torch.Tensor | None      # int64 [M, top]
+    top: torch.Tensor | None          # fp32 [M, top]
+
+
+_LOGITS = {torch.float16: B.F16, torch.bfloat16: B.BF16, torch.float32: B.F32}
+
+
+def logprobs_buffers(logits: torch.Tensor, given: int = 0, top: int = 0, entropy: bool = True) -> LogProbs:
+    """Outputs for calls of logprobs over logits of this shape, for loops that keep them."""
+    M, device = logits.shape[0], logits.device
+    real = torch.float32
+    return LogProbs(torch.empty((M, given), dtype=real, device=device) if given else None,
+                    torch.empty(M, dtype=real, device=device) if entropy else None,
+                    torch.empty((M, top), dtype=_INT64, device=device) if top else None,
+                    torch.empty((M, top), dtype=real, device=device) if top else None)
+
+
+def logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None, top: int = 0, entropy: bool = True, scale: float = 1.0,
+             out: LogProbs | None = None) -> LogProbs:
+    """rosaq_logprobs of logits [M, V] (fp16, bf16 or fp32): of tokens int64 [M, given], or [M] for one of each row (below zero: padding), and
+    of the `top` largest, with the entropy.  out (logprobs_buffers) says instead of `entropy` whether that is wanted."""
+    M, V = logits.shape
+    if logits.dtype not in _LOGITS:
+        raise ValueError("logits must be fp16, bf16 or fp32")
+    d = B.LogprobsDesc()
+    d.M, d.V, d.type, d.scale, d.top = M, V, _LOGITS[logits.dtype], scale, top
+    d.logits, d.ld = logits.data_ptr(), _row_stride("logits", logits, M, V, logits.dtype)
+    given = 0
+    if tokens is not None:
+        if tokens.dim() not in (1, 2) or tokens.shape[0] != M:
+            raise ValueError(f"tokens must be [{M}, given] or [{M}]")
+        given = 1 if tokens.dim() == 1 else tokens.shape[1]
+        d.given, d.tokens = given, _integers("tokens", tokens, _INT64, M * given)
+    if out is None:
+        out = logprobs_buffers(logits, given, top, entropy)
+    for name, t, shape, dtype in (("given", out.given, (M, given) if given else None, torch.float32), ("entropy", out.entropy, (M,), torch.float32),
+                                  ("top_ids", out.top_ids, (M, top) if top else None, _INT64), ("top", out.top, (M, top) if top else None, torch.float32)):
+        if t is None:
+            if shape is not None and name != "entropy":
+                raise ValueError(f"out.{name} is missing")
+        elif t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"out.{name} must be a contiguous {dtype} tensor {list(shape or ())}")
+    d.given_out, d.entropy, d.top_ids, d.top_out = (None if t is None else t.data_ptr() for t in out)
+    device = _device_of(logits, tokens, *out)
+    if device != _current_device():
+        with torch.cuda.device(device):
+            B.rosaq_logprobs(d, _stream_on(device))
+    else:
+        B.rosaq_logprobs(d, _stream_on(device))
+    return out

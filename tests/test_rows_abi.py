@@ -57,3 +57,35 @@ def test_rmsnorm_refuses_overlap():
     # columns of one buffer are apart: the call gets to its next complaint
     assert _code(lambda: _norm(ldx=2048, y=X + 1024, ldy=2048, weight=X + 2 * 512)) == ARG
     assert _code(lambda: _norm(ldx=2048, y=X + 1008, ldy=2048)) == ARG and _code(lambda: _norm(ldx=2048, y=X + 2 * 1544, ldy=2048)) == ARG
+
+
+def _logprobs(**over):
+    d = B.LogprobsDesc()
+    for k, v in dict(dict(M=4, V=1000, type=B.F16, scale=1.0, logits=X, ld=1000, given=2, top=5, tokens=Y, given_out=Z, entropy=Z + 0x1000,
+                          top_ids=Z + 0x2000, top_out=Z + 0x3000), **over).items():
+        setattr(d, k, v)
+    return B.rosaq_logprobs(d)
+
+
+def test_logprobs_refusals():
+    assert B.lib().rosaq_logprobs(None, None) == NULL
+    for name in ("logits", "tokens", "given_out", "top_ids", "top_out"):
+        assert _code(lambda: _logprobs(**{name: 0})) == NULL, name
+    assert _code(lambda: _logprobs(given=0, top=0, entropy=0)) == NULL
+    assert _code(lambda: _logprobs(M=0)) == SHAPE and _code(lambda: _logprobs(V=0)) == SHAPE and _code(lambda: _logprobs(V=(1 << 30) + 1, ld=1 << 31)) == SHAPE
+    for given in (-1, 4097):
+        assert _code(lambda: _logprobs(given=given)) == SHAPE
+    for top in (-1, 65):
+        assert _code(lambda: _logprobs(top=top)) == SHAPE
+    assert _code(lambda: _logprobs(V=4, top=5)) == SHAPE
+    assert _code(lambda: _logprobs(ld=999)) == SHAPE and _code(lambda: _logprobs(ld=(1 << 40) + 1)) == SHAPE
+    for scale in (0.0, -1.0, float("nan"), float("inf"), 2e18, 1e-19):
+        assert _code(lambda: _logprobs(scale=scale)) == ARG
+    for kind in (-1, 3):
+        assert _code(lambda: _logprobs(type=kind)) == ARG
+    assert _code(lambda: _logprobs(logits=X + 1)) == ALIGN and _code(lambda: _logprobs(logits=X + 2, type=B.F32)) == ALIGN
+    for name, at in (("tokens", Y + 4), ("given_out", Z + 2), ("entropy", Z + 0x1001), ("top_ids", Z + 0x2004), ("top_out", Z + 0x3002)):
+        assert _code(lambda: _logprobs(**{name: at})) == ALIGN, name
+    for over in (dict(entropy=X + 7996), dict(given_out=Y + 60), dict(top_ids=X - 8), dict(top_ids=Z + 24), dict(top_out=Z + 0x1008),
+                 dict(top_out=Z + 0x2000 + 156)):
+        assert _code(lambda: _logprobs(**over)) == ARG, over
