@@ -386,6 +386,16 @@ typedef struct {
 size_t rosaq_workspace_bytes_attention(const rosaq_attention_desc* desc);
 int rosaq_attention(const rosaq_attention_desc* desc, void* ws_dev, size_t ws_bytes, void* hip_stream);
 
+/* rosaq_attention_window - rosaq_attention whose rows look back a window and to the sequence's first tokens: row i of a sequence of n rows and l
+ * cached tokens is at position p = l - n + i and sees token j <= p if j > p - window or j < sinks.  So its cost does not grow with the text, and
+ * pages between the sinks and the first row's window may be given back: their entries in pages_dev may hold any number, and nothing
+ * that lies in them reaches a result.  max_kv, kv_len_dev and pages_dev count all of a sequence's tokens from its first on, given back or not.
+ * desc as above with causal 1 and prefix_len 0 (a prefix's pages may stand in every sequence's row of pages_dev); window 1 to 2^30 (from max_kv on it is
+ * rosaq_attention), sinks 0 to 2^30.  Its workspace size is its own.  Errors: those of rosaq_attention. */
+size_t rosaq_workspace_bytes_attention_window(const rosaq_attention_desc* desc, int32_t window, int32_t sinks);
+int rosaq_attention_window(const rosaq_attention_desc* desc, int32_t window, int32_t sinks, void* ws_dev, size_t ws_bytes,
+                           void* hip_stream);
+
 /* ---- around the projections: the norm in front of them, log probabilities behind the last -------------------
  *
  * Both take whole rows.  Asynchronous on hip_stream, allocate nothing, never synchronise, need no workspace and may be captured into a

@@ -28,7 +28,7 @@ EXPORTED = ["rosaq_pack_weights", "rosaq_workspace_bytes", "rosaq_workspace_byte
             "rosaq_linear_headwise_static", "rosaq_linear_batch", "rosaq_linear_swiglu", "rosaq_mlp_swiglu", "rosaq_workspace_bytes_mlp", "rosaq_stream_probe", "rosaq_packed_clone", "rosaq_pca_headwise", "rosaq_pca_full",
             "rosaq_packed_info", "rosaq_packed_export", "rosaq_tune", "rosaq_launch_shape", "rosaq_launch_many_rows", "rosaq_block_map", "rosaq_packed_image", "rosaq_free",
             "rosaq_cache_bytes", "rosaq_rope_table", "rosaq_rope", "rosaq_cache_append", "rosaq_cache_read", "rosaq_attention", "rosaq_workspace_bytes_attention",
-            "rosaq_rmsnorm", "rosaq_logprobs", "rosaq_last_error"]
+            "rosaq_attention_window", "rosaq_workspace_bytes_attention_window", "rosaq_rmsnorm", "rosaq_logprobs", "rosaq_last_error"]
 
 
 class PackDesc(C.Structure):
@@ -157,6 +157,10 @@ def lib() -> C.CDLL:
         L.rosaq_workspace_bytes_attention.restype = sz
         L.rosaq_attention.argtypes = [C.POINTER(AttentionDesc), vp, sz, vp]
         L.rosaq_attention.restype = C.c_int
+        L.rosaq_workspace_bytes_attention_window.argtypes = [C.POINTER(AttentionDesc), i32, i32]
+        L.rosaq_workspace_bytes_attention_window.restype = sz
+        L.rosaq_attention_window.argtypes = [C.POINTER(AttentionDesc), i32, i32, vp, sz, vp]
+        L.rosaq_attention_window.restype = C.c_int
         L.rosaq_rmsnorm.argtypes = [C.POINTER(RmsNormDesc), vp]
         L.rosaq_rmsnorm.restype = C.c_int
         L.rosaq_logprobs.argtypes = [C.POINTER(LogprobsDesc), vp]
@@ -359,6 +363,17 @@ def rosaq_workspace_bytes_attention(desc: AttentionDesc) -> int:
 
 def rosaq_attention(desc: AttentionDesc, ws_ptr: int, ws_bytes: int, stream: int = 0):
     _check(lib().rosaq_attention(desc, ws_ptr, ws_bytes, stream))
+
+
+def rosaq_workspace_bytes_attention_window(desc: AttentionDesc, window: int, sinks: int) -> int:
+    n = lib().rosaq_workspace_bytes_attention_window(C.byref(desc), window, sinks)
+    if n == 0:
+        raise RosaqError(-2, rosaq_last_error())
+    return n
+
+
+def rosaq_attention_window(desc: AttentionDesc, window: int, sinks: int, ws_ptr: int, ws_bytes: int, stream: int = 0):
+    _check(lib().rosaq_attention_window(desc, window, sinks, ws_ptr, ws_bytes, stream))
 
 
 def rosaq_rmsnorm(desc: RmsNormDesc, stream: int = 0):

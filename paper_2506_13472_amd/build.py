@@ -15,7 +15,8 @@ OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "librosaq.so")
 HOST_SOURCES = ["rosaq_pack.cpp", "rosaq_api.cpp", "rosaq_attention.cpp", "rosaq_rows.cpp"]
 HIP_SOURCES = ["rosaq_kernels.hip", "rosaq_pca.hip", "rosaq_static.hip", "rosaq_quant.hip", "rosaq_rotate.hip",
-               "rosaq_wide.hip", "rosaq_cache.hip", "rosaq_attention.hip", "rosaq_norm.hip", "rosaq_logprobs.hip"]
+               "rosaq_wide.hip", "rosaq_cache.hip", "rosaq_attention.hip",
+               "rosaq_attention_window.hip", "rosaq_norm.hip", "rosaq_logprobs.hip"]
 
 
 def hipcc() -> str:

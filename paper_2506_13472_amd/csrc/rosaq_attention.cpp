@@ -152,6 +152,32 @@ static int check_attention(const rosaq_attention_desc* d, AttendArgs* a, bool po
   return ROSAQ_OK;
 }
 
+static int check_window(const rosaq_attention_desc& d, int32_t window, int32_t sinks, AttendArgs* a) {
+  if (window < 1 || window > (1 << 30)) return fail(ROSAQ_ERR_SHAPE, "window must be in [1, 2^30]");
+  if (sinks < 0 || sinks > (1 << 30)) return fail(ROSAQ_ERR_SHAPE, "sinks must be in [0, 2^30]");
+  if (d.causal != 1) return fail(ROSAQ_ERR_ARG, "a window is counted back from a row's own position: causal must be 1");
+  if (d.prefix_len != 0) return fail(ROSAQ_ERR_ARG, "with a window a shared prefix is part of every sequence's pages: prefix_len must be 0");
+  a->window = window;
+  a->sinks = sinks;
+  return ROSAQ_OK;
+}
+
+static size_t workspace_of(const AttendArgs& a) {
+  const AttendPlan p = plan_attention(a);
+  return p.ws_bytes < 256 ? 256 : p.ws_bytes;
+}
+
+static int attend(AttendArgs& a, void* ws_dev, size_t ws_bytes, void* hip_stream) {
+  const AttendPlan p = plan_attention(a);
+  if (p.own.grid + p.prefix.grid >= kMaxGrid) return fail(ROSAQ_ERR_SHAPE, "sequences x max_rows x q_heads too large: split the call");
+  if (p.ws_bytes) {
+    if (!ws_dev || ws_bytes < p.ws_bytes) return fail(ROSAQ_ERR_WORKSPACE, "workspace missing or too small");
+    if (misaligned(ws_dev, 256)) return fail(ROSAQ_ERR_ALIGN, "workspace must be 256-byte aligned");
+    a.part = static_cast<float*>(ws_dev);
+  }
+  return launch_attention(a, p, hip_stream);
+}
+
 }  // namespace rosaq
 
 using namespace rosaq;
@@ -248,23 +274,25 @@ int rosaq_cache_read(const rosaq_cache* cache, const int64_t* slots_dev, int32_t
 
 size_t rosaq_workspace_bytes_attention(const rosaq_attention_desc* desc) {
   AttendArgs a{};
-  if (check_attention(desc, &a, false) != ROSAQ_OK) return 0;
-  const AttendPlan p = plan_attention(a);
-  return p.ws_bytes < 256 ? 256 : p.ws_bytes;
+  return check_attention(desc, &a, false) != ROSAQ_OK ? 0 : workspace_of(a);
 }
 
 int rosaq_attention(const rosaq_attention_desc* desc, void* ws_dev, size_t ws_bytes, void* hip_stream) {
   AttendArgs a{};
   const int rc = check_attention(desc, &a, true);
-  if (rc != ROSAQ_OK) return rc;
-  const AttendPlan p = plan_attention(a);
-  if (p.own.grid + p.prefix.grid >= kMaxGrid) return fail(ROSAQ_ERR_SHAPE, "sequences x max_rows x q_heads too large: split the call");
-  if (p.ws_bytes) {
-    if (!ws_dev || ws_bytes < p.ws_bytes) return fail(ROSAQ_ERR_WORKSPACE, "workspace missing or too small");
-    if (misaligned(ws_dev, 256)) return fail(ROSAQ_ERR_ALIGN, "workspace must be 256-byte aligned");
-    a.part = static_cast<float*>(ws_dev);
-  }
-  return launch_attention(a, p, hip_stream);
+  return rc != ROSAQ_OK ? rc : attend(a, ws_dev, ws_bytes, hip_stream);
+}
+
+size_t rosaq_workspace_bytes_attention_window(const rosaq_attention_desc* desc, int32_t window, int32_t sinks) {
+  AttendArgs a{};
+  return check_attention(desc, &a, false) != ROSAQ_OK || check_window(*desc, window, sinks, &a) != ROSAQ_OK ? 0 : workspace_of(a);
+}
+
+int rosaq_attention_window(const rosaq_attention_desc* desc, int32_t window, int32_t sinks, void* ws_dev, size_t ws_bytes, void* hip_stream) {
+  AttendArgs a{};
+  int rc = check_attention(desc, &a, true);
+  if (rc == ROSAQ_OK) rc = check_window(*desc, window, sinks, &a);
+  return rc != ROSAQ_OK ? rc : attend(a, ws_dev, ws_bytes, hip_stream);
 }
 
 }  // extern "C"

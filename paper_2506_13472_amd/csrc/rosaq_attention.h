@@ -86,6 +86,7 @@ struct AttendArgs {
   int max_rows, max_kv;
   int capacity;                             // tokens of a sequence that are looked at: of max_kv, those that `pages` has room for
   int causal;
+  int window, sinks;                        // window 0: none
   float scale_log2;                         // scale * log2(e)
   int dim, bits;
   float* part;                              // partial results (AttendPlan::parts > 1)
@@ -112,5 +113,6 @@ struct AttendPlan {
 };
 AttendPlan plan_attention(const AttendArgs& a);
 int launch_attention(const AttendArgs& a, const AttendPlan& plan, void* stream);
+void launch_attention_window(const AttendArgs& a, const AttendPlan& plan, void* stream);
 
 }  // namespace rosaq

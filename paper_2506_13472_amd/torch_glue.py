@@ -199,8 +199,11 @@ class AttentionPlan:
     need more).  Calls with one plan must not overlap in time."""
 
     def __init__(self, cache: KvCache, q_heads: int, sequences: int, max_kv: int, max_rows: int = 1, rows: int | None = None,
-                 prefix_len: int = 0, causal: bool = True, scale: float | None = None):
-        """`rows`: rows of q, sequences * max_rows unless given; scale: head_dim^-1/2 unless given."""
+                 prefix_len: int = 0, causal: bool = True, scale: float | None = None, window: int | None = None, sinks: int = 0):
+        """`rows`: rows of q, sequences * max_rows unless given; scale: head_dim^-1/2 unless given.  With `window` a row sees that many
+        tokens, its own among them, and the sequence's first `sinks` (rosaq_attention_window)."""
+        if window is None and sinks:
+            raise ValueError("sinks are those of a window: window is missing")
         self.cache = cache
         self.M, self.width, self.sequences, self.prefix_len = sequences * max_rows if rows is None else rows, q_heads * cache.head_dim, sequences, prefix_len
         self.desc = B.AttentionDesc()
@@ -208,13 +211,15 @@ class AttentionPlan:
         d.cache = C.pointer(cache.args)
         d.q_heads, d.M, d.sequences, d.max_kv, d.max_rows, d.prefix_len = q_heads, self.M, sequences, max_kv, max_rows, prefix_len
         d.causal, d.scale = int(causal), cache.head_dim ** -0.5 if scale is None else scale
-        self.ws = torch.empty(B.rosaq_workspace_bytes_attention(d), dtype=torch.uint8, device=cache.data.device)
+        self.window, self.sinks = window, sinks
+        need = B.rosaq_workspace_bytes_attention(d) if window is None else B.rosaq_workspace_bytes_attention_window(d, window, sinks)
+        self.ws = torch.empty(need, dtype=torch.uint8, device=cache.data.device)
         self.ws_bytes = self.ws.numel()
 
 
 def attention(plan: AttentionPlan, q: torch.Tensor, kv_len: torch.Tensor, pages: torch.Tensor, row_start: torch.Tensor | None = None,
               prefix_pages: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
-    """rosaq_attention: q [rows, q_heads * head_dim], kv_len int32 [sequences], pages int32 [sequences, pages of a sequence],
+    """rosaq_attention, or rosaq_attention_window where the plan has a window: q [rows, q_heads * head_dim], kv_len int32 [sequences], pages int32 [sequences, pages of a sequence],
     row_start int32 [sequences + 1] (without it sequence b has row b), prefix_pages int32.  out must not overlap q; without it,
     rows that belong to no sequence are zero."""
     d, M = plan.desc, plan.M
@@ -241,7 +246,10 @@ def attention(plan: AttentionPlan, q: torch.Tensor, kv_len: torch.Tensor, pages:
     d.ldy = _ld("out", y, M, plan.width)
     d.q, d.ldq, d.y = q.data_ptr(), ldq, y.data_ptr()
     d.kv_len, d.pages, d.page_stride, d.row_start, d.prefix_pages = at_len, at_pages, pages.size(1), at_rows, at_prefix
-    B.rosaq_attention(d, plan.ws.data_ptr(), plan.ws_bytes, _stream_on(device))
+    if plan.window is None:
+        B.rosaq_attention(d, plan.ws.data_ptr(), plan.ws_bytes, _stream_on(device))
+    else:
+        B.rosaq_attention_window(d, plan.window, plan.sinks, plan.ws.data_ptr(), plan.ws_bytes, _stream_on(device))
     return y
 
 
