@@ -398,7 +398,7 @@ int rosaq_attention_window(const rosaq_attention_desc* desc, int32_t window, int
 
 /* ---- around the projections: the norm in front of them, log probabilities behind the last -------------------
  *
- * Both take whole rows.  Asynchronous on hip_stream, allocate nothing, never synchronise, need no workspace and may be captured into a
+ * Both take whole rows.  Asynchronous on hip_stream, allocate nothing, never synchronise and may be captured into a
  * graph; the current device must be the one that holds the memory. */
 
 #define ROSAQ_F16  0
@@ -451,8 +451,12 @@ typedef struct {
   float* top_out_dev;                /* DEVICE [M x top], NULL with top 0                                */
 } rosaq_logprobs_desc;
 
-/* Outputs overlap nothing.  Errors: NULL, SHAPE, ARG (type, scale, overlap), ALIGN, HIP. */
-int rosaq_logprobs(const rosaq_logprobs_desc* desc, void* hip_stream);
+/* Outputs overlap nothing.  ws_dev: DEVICE scratch, 256-byte aligned, that needs no initialisation, or NULL.  With rosaq_workspace_bytes_logprobs(desc)
+ * bytes (a matter of M, V and top; pointers may still be NULL) few long rows are shared by several workgroups each; with less the call takes longer and its
+ * sums are added in another order.  Calls that share a workspace must not overlap in time.
+ * Errors: NULL, SHAPE, ARG (type, scale, overlap), ALIGN, HIP (workspace_bytes: 0 on any). */
+size_t rosaq_workspace_bytes_logprobs(const rosaq_logprobs_desc* desc);
+int rosaq_logprobs(const rosaq_logprobs_desc* desc, void* ws_dev, size_t ws_bytes, void* hip_stream);
 
 /* rosaq_stream_probe - measurement aid, no arithmetic of the method: one launch of
  * `workgroups` x `threads` in which every wave reads its own contiguous share of

@@ -28,7 +28,8 @@ EXPORTED = ["rosaq_pack_weights", "rosaq_workspace_bytes", "rosaq_workspace_byte
             "rosaq_linear_headwise_static", "rosaq_linear_batch", "rosaq_linear_swiglu", "rosaq_mlp_swiglu", "rosaq_workspace_bytes_mlp", "rosaq_stream_probe", "rosaq_packed_clone", "rosaq_pca_headwise", "rosaq_pca_full",
             "rosaq_packed_info", "rosaq_packed_export", "rosaq_tune", "rosaq_launch_shape", "rosaq_launch_many_rows", "rosaq_block_map", "rosaq_packed_image", "rosaq_free",
             "rosaq_cache_bytes", "rosaq_rope_table", "rosaq_rope", "rosaq_cache_append", "rosaq_cache_read", "rosaq_attention", "rosaq_workspace_bytes_attention",
-            "rosaq_attention_window", "rosaq_workspace_bytes_attention_window", "rosaq_rmsnorm", "rosaq_logprobs", "rosaq_last_error"]
+            "rosaq_attention_window", "rosaq_workspace_bytes_attention_window", "rosaq_rmsnorm", "rosaq_logprobs", "rosaq_workspace_bytes_logprobs",
+            "rosaq_last_error"]
 
 
 class PackDesc(C.Structure):
@@ -163,7 +164,9 @@ def lib() -> C.CDLL:
         L.rosaq_attention_window.restype = C.c_int
         L.rosaq_rmsnorm.argtypes = [C.POINTER(RmsNormDesc), vp]
         L.rosaq_rmsnorm.restype = C.c_int
-        L.rosaq_logprobs.argtypes = [C.POINTER(LogprobsDesc), vp]
+        L.rosaq_workspace_bytes_logprobs.argtypes = [C.POINTER(LogprobsDesc)]
+        L.rosaq_workspace_bytes_logprobs.restype = sz
+        L.rosaq_logprobs.argtypes = [C.POINTER(LogprobsDesc), vp, sz, vp]
         L.rosaq_logprobs.restype = C.c_int
         L.rosaq_free.argtypes = [vp]
         L.rosaq_free.restype = None
@@ -380,8 +383,15 @@ def rosaq_rmsnorm(desc: RmsNormDesc, stream: int = 0):
     _check(lib().rosaq_rmsnorm(desc, stream))
 
 
-def rosaq_logprobs(desc: LogprobsDesc, stream: int = 0):
-    _check(lib().rosaq_logprobs(desc, stream))
+def rosaq_workspace_bytes_logprobs(desc: LogprobsDesc) -> int:
+    n = lib().rosaq_workspace_bytes_logprobs(C.byref(desc))
+    if n == 0:
+        raise RosaqError(-2, rosaq_last_error())
+    return n
+
+
+def rosaq_logprobs(desc: LogprobsDesc, ws_ptr: int = 0, ws_bytes: int = 0, stream: int = 0):
+    _check(lib().rosaq_logprobs(desc, ws_ptr, ws_bytes, stream))
 
 
 def rosaq_stream_probe(src_ptr: int, src_bytes: int, shared_ptr: int, shared_bytes: int,

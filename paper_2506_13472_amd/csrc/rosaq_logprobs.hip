@@ -6,13 +6,15 @@
 // in which no large numbers cancel: both terms of H are positive, and x - m is taken before it is multiplied.
 //
 // The alternatives need no second look at the row but at a few pieces of it.  Every thread also keeps the largest logit of its share (every
-// THREADS-th piece of 16 bytes) and where that was.  Of 256 groups of threads the top-th largest is a bound that at least `top` logits
-// reach, and logits that reach it lie only in the shares of threads whose largest does: about `top` shares of a THREADS-th of the row.  Those are read
+// THREADS-th piece of 16 bytes) and where that was.  Of 256 groups of threads the top-th largest (or some of those next to it) is a bound that at least
+// `top` logits reach, and only in the shares of threads whose largest does: about `top` shares of a THREADS-th of the row.  Those are read
 // again (from a cache, mostly), what reaches the bound goes to a list in LDS, and every member counts how many are before it.
+// A bound without a search, the least of `top` groups' largest, lets three times as many logits through, and cost more on the list than the search
+// (64 rows of 32000, five of each: 11.2 us against 8.5).
 //
 // Order is by value and of equal values by the lower index, so that the answer does not depend on who finds what when.  The bound is of the same order: a
 // value, and the last piece in which that value counts.  A row of one value throughout (or of few logits and -inf besides) so has a short list too.
-// Where the list would be longer than its place, which takes a row whose largest logits all lie in few threads' shares, the bound is
+// Where the list would be longer than its place, which takes a row whose largest logits nearly all lie in few threads' shares, the bound is
 // found by bisection over the whole row.
 #include <hip/hip_runtime.h>
 
@@ -20,12 +22,13 @@
 #include <string>
 
 #include "rosaq_gemm.h"
+#include "rosaq_reduce.h"
 #include "rosaq_rows.h"
 
 namespace rosaq {
 
 constexpr int kGroups = 256;        // of threads, over which the bound is found
-constexpr int kList = 1024;         // logits that reach it, at most
+constexpr int kList = 1024;         // logits on the list, at most
 
 // One type of logits: elements of a 16-byte piece, the low bits of a key (below) that say nothing, and words of -inf.
 struct Half {
@@ -62,11 +65,6 @@ __device__ __forceinline__ Sums moved(const Sums& a, float m, float c) {
   const float d = larger((a.m - m) * c, kLeast), f = __builtin_amdgcn_exp2f(d);
   return Sums{m, a.s * f, f * __builtin_fmaf(a.s, d, a.t)};
 }
-__device__ __forceinline__ Sums joined(const Sums& a, const Sums& b, float c) {
-  const float m = larger(a.m, b.m);
-  const Sums x = moved(a, m, c), y = moved(b, m, c);
-  return Sums{m, x.s + y.s, x.t + y.t};
-}
 
 // A row, cut into pieces of 16 bytes at 16-byte addresses; the first and last may be partly of the row.
 template <class K> struct Row {
@@ -87,85 +85,130 @@ template <class K> struct Row {
     else if constexpr (K::kShift == 16) return __builtin_bit_cast(float, j % 2 ? (&w.x)[j / 2] & 0xffff0000u : (&w.x)[j / 2] << 16);
     else return __builtin_bit_cast(float, (&w.x)[j]);
   }
-  // f(element, index) for those of a piece that are the row's
-  template <class F> __device__ __forceinline__ void each(int piece, F f) const {
+  // Of any piece: -inf in place of what is not the row's; the places (bits) of those that are.
+  __device__ __forceinline__ uint32_t load_any(int piece, uint4* w) const {
     if (whole(piece)) {
-      const uint4 w = load(piece);
-#pragma unroll
-      for (int j = 0; j < K::kEach; ++j) f(element(w, j), index(piece, j));
-    } else {
-      for (int j = 0; j < K::kEach; ++j) {
-        const int at = index(piece, j);
-        if (at >= 0 && at < length) f(static_cast<float>(first[at]), at);
-      }
+      *w = load(piece);
+      return (1u << K::kEach) - 1;
     }
+    uint32_t to[4] = {K::kNone, K::kNone, K::kNone, K::kNone}, there = 0;
+#pragma unroll
+    for (int j = 0; j < K::kEach; ++j) {
+      const int at = index(piece, j);
+      if (at < 0 || at >= length) continue;
+      there |= 1u << j;
+      if constexpr (K::kEach == 4) to[j] = __builtin_bit_cast(uint32_t, first[at]);
+      else to[j / 2] = j % 2 ? (to[j / 2] & 0xffffu) | static_cast<uint32_t>(__builtin_bit_cast(uint16_t, first[at])) << 16
+                             : (to[j / 2] & 0xffff0000u) | __builtin_bit_cast(uint16_t, first[at]);
+    }
+    *w = make_uint4(to[0], to[1], to[2], to[3]);
+    return there;
   }
 };
 
-// What a bound is: logits of a larger key, and those of its key in pieces up to `piece`.  Keys without their low bits.
-struct Bound {
-  uint32_t key;
-  int piece;
-  __device__ __forceinline__ bool reached(uint32_t k, int p) const { return k > key || (k == key && p <= piece); }
-};
+// A bound: a key without its low bits, and of logits of that key the last piece that counts.  As one number, the larger the fewer reach it.
+typedef uint64_t Bound;
+__device__ __forceinline__ Bound bound_of(uint32_t key, int piece) { return static_cast<uint64_t>(key) << 32 | ~static_cast<uint32_t>(piece); }
 
-// The largest number of BITS bits that, as `count` says, at least n reach; or one that n reach and no more.
-template <int BITS, class F> __device__ __forceinline__ uint32_t largest(int n, F count) {
+// A number of BITS bits that, as `count` says, at least n reach and no more than n + slack, or, where equal numbers leave none, the largest that n reach.
+template <int BITS, class F> __device__ __forceinline__ uint32_t reached_by(int n, int slack, F count) {
   uint32_t v = 0;
+#pragma unroll 1
   for (int bit = BITS - 1; bit >= 0; --bit) {
     const int reach = count(v | 1u << bit);
     if (reach >= n) v |= 1u << bit;
-    if (reach == n) break;
+    if (reach >= n && reach <= n + slack) break;
   }
   return v;
 }
 
-__device__ __forceinline__ int wave_sum(int v) {
+// A logit and where it is, ordered as the alternatives are.
+__device__ __forceinline__ uint64_t member_of(uint32_t key, int at) { return static_cast<uint64_t>(key) << 32 | ~static_cast<uint32_t>(at); }
+__device__ __forceinline__ int index_of(uint64_t member) { return static_cast<int>(~static_cast<uint32_t>(member)); }
+
+// How many of a list in LDS (in pairs, behind its n members zeros up to a multiple of eight) are before this one.
+__device__ __forceinline__ int rank_of(uint64_t member, const ulonglong2* list, int n) {
+  int before = 0;
+#pragma unroll 1
+  for (int o = 0; o < n; o += 8) {
+    ulonglong2 w[4];
 #pragma unroll
-  for (int n = 1; n < 64; n *= 2) v += __shfl_xor(v, n, 64);
-  return v;
+    for (int u = 0; u < 4; ++u) w[u] = list[o / 2 + u];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) before += (w[u].x > member) + (w[u].y > member);
+  }
+  return before;
 }
 
-template <class K, int THREADS, bool TOP>
+// The sums of a workgroup's waves, from LDS to all threads.
+template <int N> __device__ __forceinline__ Sums sums_of(const float (&m)[N], const float (&s)[N], const float (&t)[N], float c) {
+  const int w = threadIdx.x % N;
+  Sums a = moved(Sums{m[w], s[w], t[w]}, row_all<N>(m[w], larger), c);
+  a.s = row_all<N>(a.s, added<float>);
+  a.t = row_all<N>(a.t, added<float>);
+  return a;
+}
+
+// What a row's sums say.
+struct Answer {
+  float m, scale, log2_s, share;       // share: T / S
+  __device__ Answer(const Sums& a, float scale) : m(a.m), scale(scale), log2_s(log2f(a.s)), share(a.t / a.s) {}
+  __device__ __forceinline__ float log_p(float x) const { return (x - m) * scale - log2_s * 0.6931471805599453f; }
+  __device__ __forceinline__ float entropy() const { return (log2_s - share) * 0.6931471805599453f; }
+};
+// The given tokens of a row, in two steps, so that nothing waits for them: `step` threads take them in turn, and the first round's are fetched ahead.
+template <class K> __device__ __forceinline__ int64_t token_of(const LogprobArgs& a, int64_t row, int g) { return g < a.given ? a.tokens[row * a.given + g] : -1; }
+template <class K> __device__ __forceinline__ float logit_of(const LogprobArgs& a, const Row<K>& x, int64_t token) {
+  return token >= 0 && token < a.V ? static_cast<float>(x.first[token]) : NAN;
+}
+template <class K>
+__device__ __forceinline__ void give(const LogprobArgs& a, int64_t row, const Row<K>& x, const Answer& y, int g, int step, int64_t token, float logit) {
+  while (g < a.given) {
+    a.given_out[row * a.given + g] = token < 0 ? 0.f : y.log_p(logit);
+    g += step;
+    token = token_of<K>(a, row, g);
+    logit = logit_of(a, x, token);
+  }
+}
+
+// Results of the parts of a row (SPLIT), of part p of row r at r parts + p: sums, then the alternatives' members, largest first, 0 behind them.
+struct Parts {
+  float4* sums;
+  uint64_t* members;
+  __device__ Parts(const LogprobArgs& a) : sums(static_cast<float4*>(a.ws)), members(reinterpret_cast<uint64_t*>(sums + static_cast<int64_t>(a.M) * a.parts)) {}
+};
+
+template <class K, int THREADS, bool TOP, bool SPLIT>
 __global__ __launch_bounds__(THREADS) void logprobs_kernel(LogprobArgs a) {
-  constexpr int E = K::kEach, kWaves = THREADS / 64, kAhead = 4, kBits = 32 - K::kShift, kLanes = THREADS / kGroups;
-  constexpr int kMember = TOP ? kList : 1, kGroup = TOP ? kGroups : 1, kShare = TOP ? THREADS : 1;
+  constexpr int E = K::kEach, kWaves = THREADS / 64, kAhead = 4, kBits = 32 - K::kShift;
   __shared__ float lds_m[kWaves], lds_s[kWaves], lds_t[kWaves];
-  __shared__ uint32_t group_key[kGroup];
-  __shared__ int group_piece[kGroup];
-  __shared__ int share[kShare];              // threads whose share holds logits that reach the bound
-  __shared__ uint32_t member_key[kMember];
-  __shared__ int member_at[kMember];
-  __shared__ Bound bound;
+  __shared__ Bound group[TOP ? kGroups : 1], lds_bound;
+  __shared__ int share[TOP ? THREADS : 1];   // threads whose share holds logits that reach the bound
+  __shared__ ulonglong2 list[TOP ? kList / 2 + 4 : 1];
   __shared__ int shares, members, count;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const float c = a.scale * 1.4426950408889634f;
-  for (int64_t row = blockIdx.x; row < a.M; row += gridDim.x) {
+  uint64_t* const member = reinterpret_cast<uint64_t*>(list);
+  const int64_t tasks = SPLIT ? static_cast<int64_t>(a.M) * a.parts : a.M;
+  for (int64_t task = blockIdx.x; task < tasks; task += gridDim.x) {
+    const int64_t row = SPLIT ? task / a.parts : task;
     const Row<K> x(a, row);
+    // the pieces of this workgroup, and those of them that are whole
+    const int each = SPLIT ? (x.pieces + a.parts - 1) / a.parts : x.pieces, lo = SPLIT ? static_cast<int>(task % a.parts) * each : 0;
+    const int hi = min(lo + each, x.pieces), turns = (each + THREADS - 1) / THREADS;
+    const int first = lo == 0 && !x.whole(0) ? 1 : lo, end = hi == x.pieces && first < hi && !x.whole(hi - 1) ? hi - 1 : hi;
     Sums sums{kLowest, 0.f, 0.f};
     uint32_t best_key = 0;                   // of this thread's share: the largest, 0 without one, and the first piece that holds it
-    int best_piece = tid;
-    auto seen = [&](float most, int piece) {
-      if constexpr (TOP) {
-        const uint32_t k = key_of(most);
-        if (k > best_key) { best_key = k; best_piece = piece; }
-      }
-    };
+    int best_piece = lo + tid;
+    Bound best = 0;                          // the two as one
     auto add = [&](float v) {
-      const float d = larger((v - sums.m) * c, kLeast), e = __builtin_amdgcn_exp2f(d);
+      const float d = fmaxf((v - sums.m) * c, kLeast), e = __builtin_amdgcn_exp2f(d);
       sums.s += e;
       sums.t = __builtin_fmaf(e, d, sums.t);
     };
-    auto part = [&](int piece) {             // one that is partly of the row
-      x.each(piece, [&](float v, int) {
-        seen(v, piece);
-        sums = moved(sums, larger(sums.m, v), c);
-        add(v);
-      });
-    };
-    const int last = x.pieces - 1, end = x.whole(last) ? x.pieces : last;
-    if (tid == 0 && !x.whole(0)) part(0);
-    for (int p0 = tid ? tid : (x.whole(0) ? 0 : THREADS); p0 < end; p0 += kAhead * THREADS) {
+    const int g = tid - (THREADS - 64);      // the last wave answers for the given tokens
+    const int64_t token = !SPLIT && g >= 0 ? token_of<K>(a, row, g) : -1;
+    for (int p0 = lo + tid < first ? lo + tid + THREADS : lo + tid; p0 < end; p0 += kAhead * THREADS) {
       uint4 w[kAhead];
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
@@ -178,7 +221,10 @@ __global__ __launch_bounds__(THREADS) void logprobs_kernel(LogprobArgs a) {
         float top = x.element(w[u], 0);
 #pragma unroll
         for (int j = 1; j < E; ++j) top = larger(top, x.element(w[u], j));
-        if (p0 + u * THREADS < end) seen(top, p0 + u * THREADS);
+        if constexpr (TOP) {
+          const uint32_t k = key_of(top);
+          if (k > best_key && p0 + u * THREADS < end) { best_key = k; best_piece = p0 + u * THREADS; }
+        }
         most = larger(most, top);
       }
       sums = moved(sums, most, c);
@@ -187,127 +233,229 @@ __global__ __launch_bounds__(THREADS) void logprobs_kernel(LogprobArgs a) {
 #pragma unroll
         for (int j = 0; j < E; ++j) add(x.element(w[u], j));
     }
-    if (end == last && last > 0 && tid == last % THREADS) part(last);
+    // pieces that are partly of the row: its first and its last
+#pragma unroll 1
+    for (int p = lo; p < hi; p = p < hi - 1 ? hi - 1 : hi) {
+      if (x.whole(p) || tid != (p - lo) % THREADS) continue;
+      uint4 w;
+      x.load_any(p, &w);
+      float top = x.element(w, 0);
 #pragma unroll
-    for (int n = 1; n < 64; n *= 2)
-      sums = joined(sums, Sums{__shfl_xor(sums.m, n, 64), __shfl_xor(sums.s, n, 64), __shfl_xor(sums.t, n, 64)}, c);
+      for (int j = 1; j < E; ++j) top = larger(top, x.element(w, j));
+      if constexpr (TOP) {
+        const uint32_t k = key_of(top);
+        if (k > best_key || (k == best_key && p < best_piece)) { best_key = k; best_piece = p; }
+      }
+      sums = moved(sums, larger(sums.m, top), c);
+#pragma unroll
+      for (int j = 0; j < E; ++j) add(x.element(w, j));
+    }
+    const float logit = logit_of(a, x, token);
+    sums = moved(sums, wave_all(sums.m, larger), c);
+    sums.s = wave_all(sums.s, added<float>);
+    sums.t = wave_all(sums.t, added<float>);
     if (lane == 0) { lds_m[wave] = sums.m; lds_s[wave] = sums.s; lds_t[wave] = sums.t; }
     if constexpr (TOP) {
-      best_key >>= K::kShift;
-      uint32_t k = best_key;
-      int p = best_piece;
+      best = best_key ? bound_of(best_key >> K::kShift, best_piece) : 0;
+      Bound most = best;
 #pragma unroll
-      for (int n = 1; n < kLanes; n *= 2) {
-        const uint32_t ok = __shfl_xor(k, n, 64);
-        const int op = __shfl_xor(p, n, 64);
-        if (ok > k || (ok == k && op < p)) { k = ok; p = op; }
-      }
-      if (tid % kLanes == 0) { group_key[tid / kLanes] = k; group_piece[tid / kLanes] = p; }
+      for (int n = 1; n < THREADS / kGroups; n *= 2) most = max(most, __shfl_xor(most, n, 64));
+      if (tid % (THREADS / kGroups) == 0) group[tid / (THREADS / kGroups)] = most;
       if (tid == 0) { shares = 0; members = 0; }
     }
     __syncthreads();
-    sums = Sums{lds_m[0], lds_s[0], lds_t[0]};
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) sums = joined(sums, Sums{lds_m[w], lds_s[w], lds_t[w]}, c);
-    const float log2_s = log2f(sums.s);
-    const float ln_s = log2_s * 0.6931471805599453f;
-    auto log_p = [&](float v) { return (v - sums.m) * a.scale - ln_s; };
-    if (a.entropy && tid == 0) a.entropy[row] = (log2_s - sums.t / sums.s) * 0.6931471805599453f;
-    for (int g = tid; g < a.given; g += THREADS) {
-      const int64_t token = a.tokens[row * a.given + g];
-      a.given_out[row * a.given + g] = token < 0 ? 0.f : (token >= a.V ? NAN : log_p(static_cast<float>(x.first[token])));
+    sums = sums_of(lds_m, lds_s, lds_t, c);
+    const Answer answer(sums, a.scale);
+    if constexpr (SPLIT) {
+      if (tid == 0) Parts(a).sums[task] = make_float4(sums.m, sums.s, sums.t, 0.f);
     }
     if constexpr (TOP) {
       if (wave == 0) {
-        uint32_t k[kGroups / 64];
-        int p[kGroups / 64];
+        uint32_t k[kGroups / 64], p[kGroups / 64];
 #pragma unroll
-        for (int i = 0; i < kGroups / 64; ++i) { k[i] = group_key[i * 64 + lane]; p[i] = group_piece[i * 64 + lane]; }
+        for (int i = 0; i < kGroups / 64; ++i) {
+          const Bound g = group[i * 64 + lane];
+          k[i] = static_cast<uint32_t>(g >> 32);
+          p[i] = static_cast<uint32_t>(g);
+        }
+        uint32_t lane_most = k[0];
+#pragma unroll
+        for (int i = 1; i < kGroups / 64; ++i) lane_most = max(lane_most, k[i]);
+        const uint32_t most = wave_all(lane_most, [](uint32_t a, uint32_t b) { return max(a, b); });
+        // groups that reach a key; for few alternatives four of them are counted as one, which lets hardly more through and takes half as long
+        const bool few = a.top <= 32;
         auto at_least = [&](uint32_t v) {
-          int n = 0;
+          if (v > most) return 0;
+          int n = __popcll(__ballot(lane_most >= v));
+          if (few) return n;
+          n = 0;
 #pragma unroll
           for (int i = 0; i < kGroups / 64; ++i) n += __popcll(__ballot(k[i] >= v));
           return n;
         };
-        // a row of few pieces has fewer groups than alternatives: all of it is on the list
-        const uint32_t key = largest<kBits>(a.top, at_least);
-        auto up_to = [&](uint32_t last) {    // groups that reach (key, last)
-          int n = 0;
+        // a row of few pieces has fewer groups than alternatives: all of it is on the list.  A few groups too many cost less than to tell them apart
+        const uint32_t key = reached_by<kBits>(a.top, 16, at_least);
+        uint32_t last = 0;
+        if (key != 0 && at_least(key) > a.top + 24)
+          last = reached_by<32>(a.top, 16, [&](uint32_t v) {
+            int n = 0;
 #pragma unroll
-          for (int i = 0; i < kGroups / 64; ++i) n += __popcll(__ballot(k[i] > key || (k[i] == key && static_cast<uint32_t>(p[i]) <= last)));
-          return n;
-        };
-        int piece = 0x7fffffff;
-        // some more than `top` cost less on the list than here
-        if (key != 0 && at_least(key) > a.top + 64) piece = 0x7fffffff - static_cast<int>(largest<31>(a.top, [&](uint32_t v) { return up_to(0x7fffffffu - v); }));
-        if (lane == 0) bound = Bound{key, piece};
+            for (int i = 0; i < kGroups / 64; ++i) n += __popcll(__ballot(k[i] > key || (k[i] == key && p[i] >= v)));
+            return n;
+          });
+        if (lane == 0) lds_bound = static_cast<uint64_t>(key) << 32 | last;
       }
       __syncthreads();
-      Bound b = bound;
-      const int turns = (x.pieces + THREADS - 1) / THREADS;
-      if (tid < x.pieces && b.reached(best_key, best_piece)) share[atomicAdd(&shares, 1)] = tid;
+      Bound b = lds_bound;
+      if (best >= b && best) share[atomicAdd(&shares, 1)] = tid;
       __syncthreads();
-      const int n_shares = shares;
-      auto gather = [&](int s, int turn) {
-        const int piece = share[s] + turn * THREADS;
-        if (piece >= x.pieces) return;
-        x.each(piece, [&](float v, int at) {
-          const uint32_t k = key_of(v);
-          if (!b.reached(k >> K::kShift, piece)) return;
-          const int m = atomicAdd(&members, 1);
-          if (m < kList) { member_key[m] = k; member_at[m] = at; }
-        });
-      };
-      for (int i = tid; i < n_shares * turns; i += THREADS) gather(i % n_shares, i / n_shares);
-      __syncthreads();
-      if (members > kList) {
-        // counts over the whole row, of logits that reach a bound
+      int n_shares = shares, log_lanes = turns > 8 ? 4 : 3;     // threads of a share
+#pragma unroll 1
+      while (true) {
+        const uint32_t least = static_cast<uint32_t>(b >> 32);
+        const int lanes = 1 << log_lanes;
+#pragma unroll 1
+        for (int s = tid >> log_lanes; s < n_shares; s += THREADS >> log_lanes) {
+#pragma unroll 1
+          for (int p = lo + share[s] + (tid & (lanes - 1)) * THREADS; p < hi; p += lanes * THREADS) {
+            // all of a piece's logits that reach the bound take their places on the list at once
+            const bool with = bound_of(least, p) >= b;          // those of that key too
+            uint4 w;
+            const uint32_t there = x.load_any(p, &w);
+            uint32_t key[E], hits = 0;
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+              key[j] = key_of(x.element(w, j));
+              const uint32_t k = key[j] >> K::kShift;
+              hits |= (k > least || (k == least && with) ? 1u : 0u) << j;
+            }
+            hits &= there;
+            if (hits == 0) continue;
+            int m = atomicAdd(&members, __popc(hits));
+#pragma unroll
+            for (int j = 0; j < E; ++j)
+              if (hits >> j & 1) {
+                if (m < kList) member[m] = member_of(key[j], x.index(p, j));
+                ++m;
+              }
+          }
+        }
+        __syncthreads();
+        if (members <= kList) break;
+        // counts over all pieces, of logits that reach a bound
         auto count_of = [&](Bound o) {
           __syncthreads();
           if (tid == 0) count = 0;
           __syncthreads();
           int n = 0;
-          for (int p = tid; p < x.pieces; p += THREADS) x.each(p, [&](float v, int) { n += o.reached(key_of(v) >> K::kShift, p); });
-          n = wave_sum(n);
+#pragma unroll 1
+          for (int p = lo + tid; p < hi; p += THREADS) {
+            uint4 w;
+            const uint32_t there = x.load_any(p, &w);
+#pragma unroll
+            for (int j = 0; j < E; ++j) n += (there >> j & 1) && bound_of(key_of(x.element(w, j)) >> K::kShift, p) >= o;
+          }
+          n = wave_all(n, [](int a, int b) { return a + b; });
           if (lane == 0) atomicAdd(&count, n);
           __syncthreads();
           return count;
         };
-        b.key = largest<kBits>(a.top, [&](uint32_t v) { return count_of(Bound{v, 0x7fffffff}); });
-        b.piece = 0x7fffffff - static_cast<int>(largest<31>(a.top, [&](uint32_t v) { return count_of(Bound{b.key, static_cast<int>(0x7fffffffu - v)}); }));
+        const uint32_t key = reached_by<kBits>(a.top, 64, [&](uint32_t v) { return count_of(bound_of(v, -1)); });
+        b = static_cast<uint64_t>(key) << 32 | reached_by<32>(a.top, 64, [&](uint32_t v) { return count_of(static_cast<uint64_t>(key) << 32 | v); });
         __syncthreads();
-        if (tid == 0) { members = 0; shares = 0; }
-        __syncthreads();
-        if (tid < x.pieces) share[atomicAdd(&shares, 1)] = tid;
-        __syncthreads();
-        const int all = shares;
-        for (int i = tid; i < all * turns; i += THREADS) gather(i % all, i / all);
+        if (tid == 0) members = 0;
+        share[tid] = tid;
+        n_shares = THREADS;
         __syncthreads();
       }
       const int n = min(members, kList);
+      if (tid < 8) member[n + tid] = 0;
+      __syncthreads();
       for (int i = tid; i < n; i += THREADS) {
-        const uint32_t k = member_key[i];
-        const int at = member_at[i];
-        int before = 0;
-        for (int o = 0; o < n; ++o) before += member_key[o] > k || (member_key[o] == k && member_at[o] < at);
-        if (before < a.top) {
-          a.top_ids[row * a.top + before] = at;
-          a.top_out[row * a.top + before] = log_p(of_key(k));
+        const uint64_t mine = member[i];
+        const int before = rank_of(mine, list, n);
+        if (before >= a.top) continue;
+        if constexpr (SPLIT) {
+          Parts(a).members[task * a.top + before] = mine;
+        } else {
+          a.top_ids[row * a.top + before] = index_of(mine);
+          a.top_out[row * a.top + before] = answer.log_p(of_key(static_cast<uint32_t>(mine >> 32)));
         }
       }
+      if constexpr (SPLIT)
+        for (int i = n + tid; i < a.top; i += THREADS) Parts(a).members[task * a.top + i] = 0;
+    }
+    if constexpr (!SPLIT) {
+      if (a.entropy && g == 0) a.entropy[row] = answer.entropy();
+      if (g >= 0) give(a, row, x, answer, g, 64, token, logit);
     }
     __syncthreads();                         // the next row uses the same LDS
   }
 }
 
-template <class K, int THREADS> static void run(const LogprobArgs& a, hipStream_t st) {
-  const unsigned grid = static_cast<unsigned>(std::min(a.M, 1 << 20));
-  if (a.top) logprobs_kernel<K, THREADS, true><<<grid, THREADS, 0, st>>>(a);
-  else logprobs_kernel<K, THREADS, false><<<grid, THREADS, 0, st>>>(a);
+// Joins the parts of a row, a workgroup each: the sums in their order, and the alternatives from those of the parts.
+template <class K> __global__ __launch_bounds__(256) void logprobs_join_kernel(LogprobArgs a) {
+  __shared__ float lds_m[kMaxParts], lds_s[kMaxParts], lds_t[kMaxParts];
+  __shared__ ulonglong2 list[kMaxTop * kMaxParts / 2 + 4];
+  uint64_t* const member = reinterpret_cast<uint64_t*>(list);
+  const int tid = threadIdx.x, n = a.parts * a.top;
+  const int64_t row = blockIdx.x;
+  const Parts in(a);
+  const float c = a.scale * 1.4426950408889634f;
+  const Row<K> x(a, row);
+  const int64_t token = token_of<K>(a, row, tid);
+  for (int i = tid; i < n; i += 256) member[i] = in.members[row * n + i];
+  if (tid < 8) member[n + tid] = 0;
+  if (tid < kMaxParts) {
+    const float4 s = tid < a.parts ? in.sums[row * a.parts + tid] : make_float4(kLowest, 0.f, 0.f, 0.f);
+    lds_m[tid] = s.x; lds_s[tid] = s.y; lds_t[tid] = s.z;
+  }
+  const float logit = logit_of(a, x, token);
+  __syncthreads();
+  const Answer answer(sums_of(lds_m, lds_s, lds_t, c), a.scale);
+  if (a.entropy && tid == 0) a.entropy[row] = answer.entropy();
+  give(a, row, x, answer, tid, 256, token, logit);
+  for (int i = tid; i < n; i += 256) {
+    const uint64_t mine = member[i];
+    if (mine == 0) continue;
+    const int before = rank_of(mine, list, n);
+    if (before >= a.top) continue;
+    a.top_ids[row * a.top + before] = index_of(mine);
+    a.top_out[row * a.top + before] = answer.log_p(of_key(static_cast<uint32_t>(mine >> 32)));
+  }
+}
+
+template <class K, int THREADS, bool SPLIT> static void run(const LogprobArgs& a, hipStream_t st) {
+  const unsigned grid = static_cast<unsigned>(std::min<int64_t>(static_cast<int64_t>(a.M) * (SPLIT ? a.parts : 1), 1 << 20));
+  if (a.top) logprobs_kernel<K, THREADS, true, SPLIT><<<grid, THREADS, 0, st>>>(a);
+  else logprobs_kernel<K, THREADS, false, SPLIT><<<grid, THREADS, 0, st>>>(a);
+}
+
+// Threads of a workgroup.  Few lanes go idle in a row of few pieces, and more workgroups of 256 than of 512 run beside each other, of which some read while
+// others look for alternatives; long rows want more loads under way.  us with 512 / 256 threads, fp16, five alternatives: 64 rows of 8000 7.2 / 6.4, of
+// 32000 9.0 / 10.3, of 131072 19.2 / 26.8; 4096 rows of 8000 53 / 24, of 32000 71 / 54; fp32, twenty: 64 of 8000 6.7 / 7.8, 4096 of 32000 112 / 135.
+static bool wide(const LogprobArgs& a) {
+  const int64_t bytes = static_cast<int64_t>(a.V) * (a.type == ROSAQ_F32 ? 4 : 2);
+  return bytes > (a.M > 640 ? 65536 : 32768);
+}
+
+// A compute unit reads some 35 GB/s alone, so that few long rows are better shared by several, at the price of another launch.  us in 1 / 2 / 4 / 8 / 16
+// parts, fp16, five alternatives: one row of 65536 10.7 / 10.5 / 9.2 / 9.6 / 10.1, of 262144 29.1 / 19.4 / 13.3 / 10.9 / 10.2; 64 of 131072 19.1 / 15.7 / 12.9 / 13.1 / 17.7;
+// 128 of 65536 12.7 / 12.8 / 13.0 / 17.3 / 25.4, of 262144 34.0 / 23.9 / 21.5 / 23.1 / 27.1; 257 of 32000 11.7 / 14.0 / 18.7 / 26.5 / 36.5.
+int parts_of_logprobs(const LogprobArgs& a) {
+  if (a.V < 65536) return 1;
+  return std::max(1, std::min({kMaxParts, a.V / 16384, 512 / a.M}));
 }
 
 template <class K> static void run(const LogprobArgs& a, hipStream_t st) {
-  run<K, 1024>(a, st);
+  if (a.parts > 1) {
+    run<K, 512, true>(a, st);
+    logprobs_join_kernel<K><<<static_cast<unsigned>(a.M), 256, 0, st>>>(a);
+  } else if (wide(a)) {
+    run<K, 512, false>(a, st);
+  } else {
+    run<K, 256, false>(a, st);
+  }
 }
 
 int launch_logprobs(const LogprobArgs& a, void* stream) {

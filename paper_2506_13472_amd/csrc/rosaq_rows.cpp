@@ -1,6 +1,7 @@
 // C ABI of the operators over whole rows: argument checks of the norm and of the log probabilities.  No arithmetic of the method happens here.
 #include "rosaq_rows.h"
 
+#include <algorithm>
 #include <cmath>
 #include <string>
 
@@ -83,7 +84,7 @@ static int check_rmsnorm(const rosaq_rmsnorm_desc* d, NormArgs* a) {
   return ROSAQ_OK;
 }
 
-static int check_logprobs(const rosaq_logprobs_desc* d, LogprobArgs* a) {
+static int check_logprobs(const rosaq_logprobs_desc* d, LogprobArgs* a, bool pointers) {
   if (!d) return fail(ROSAQ_ERR_NULL, "desc is NULL");
   if (d->M < 1) return fail(ROSAQ_ERR_SHAPE, "M must be at least 1");
   if (d->V < 1 || d->V > (1 << 30)) return fail(ROSAQ_ERR_SHAPE, "V must be in [1, 2^30]");
@@ -91,6 +92,9 @@ static int check_logprobs(const rosaq_logprobs_desc* d, LogprobArgs* a) {
   if (!(d->scale >= 0x1p-60f && d->scale <= 0x1p60f)) return fail(ROSAQ_ERR_ARG, "scale must be a number of 2^-60 to 2^60");
   if (d->given < 0 || d->given > kMaxGiven) return fail(ROSAQ_ERR_SHAPE, "given must be in [0, 4096]");
   if (d->top < 0 || d->top > kMaxTop || d->top > d->V) return fail(ROSAQ_ERR_SHAPE, "top must be in [0, 64] and at most V");
+  a->M = d->M; a->V = d->V; a->type = d->type; a->scale = d->scale; a->given = d->given; a->top = d->top;
+  a->parts = 1; a->ws = nullptr;
+  if (!pointers) return ROSAQ_OK;
   if (!d->given && !d->top && !d->entropy_dev) return fail(ROSAQ_ERR_NULL, "no output is wanted");
   if (!d->logits_dev || (d->given && (!d->tokens_dev || !d->given_out_dev)) || (d->top && (!d->top_ids_dev || !d->top_out_dev)))
     return fail(ROSAQ_ERR_NULL, "logits, or what `given` or `top` need, is NULL");
@@ -113,10 +117,10 @@ static int check_logprobs(const rosaq_logprobs_desc* d, LogprobArgs* a) {
     for (int i = 0; i < o; ++i)
       if (out[i].p && overlap(out[o], out[i], d->M)) return overlapping(out[o], out[i]);
   }
-  a->M = d->M; a->V = d->V; a->type = d->type; a->logits = d->logits_dev; a->ld = d->ld; a->scale = d->scale;
-  a->given = d->given; a->tokens = d->tokens_dev; a->given_out = d->given_out_dev;
+  a->logits = d->logits_dev; a->ld = d->ld;
+  a->tokens = d->tokens_dev; a->given_out = d->given_out_dev;
   a->entropy = d->entropy_dev;
-  a->top = d->top; a->top_ids = d->top_ids_dev; a->top_out = d->top_out_dev;
+  a->top_ids = d->top_ids_dev; a->top_out = d->top_out_dev;
   return ROSAQ_OK;
 }
 
@@ -132,10 +136,23 @@ int rosaq_rmsnorm(const rosaq_rmsnorm_desc* desc, void* hip_stream) {
   return rc != ROSAQ_OK ? rc : launch_rmsnorm(a, hip_stream);
 }
 
-int rosaq_logprobs(const rosaq_logprobs_desc* desc, void* hip_stream) {
+size_t rosaq_workspace_bytes_logprobs(const rosaq_logprobs_desc* desc) {
   LogprobArgs a{};
-  const int rc = check_logprobs(desc, &a);
-  return rc != ROSAQ_OK ? rc : launch_logprobs(a, hip_stream);
+  if (check_logprobs(desc, &a, false) != ROSAQ_OK) return 0;
+  return std::max<size_t>(256, workspace_of_logprobs(a, parts_of_logprobs(a)));
+}
+
+int rosaq_logprobs(const rosaq_logprobs_desc* desc, void* ws_dev, size_t ws_bytes, void* hip_stream) {
+  LogprobArgs a{};
+  const int rc = check_logprobs(desc, &a, true);
+  if (rc != ROSAQ_OK) return rc;
+  if (misaligned(ws_dev, 256)) return fail(ROSAQ_ERR_ALIGN, "workspace must be 256-byte aligned");
+  const int parts = parts_of_logprobs(a);
+  if (parts > 1 && ws_dev && ws_bytes >= workspace_of_logprobs(a, parts)) {
+    a.parts = parts;
+    a.ws = ws_dev;
+  }
+  return launch_logprobs(a, hip_stream);
 }
 
 }  // extern "C"

@@ -1,5 +1,6 @@
 // What the kernels of whole rows are told: the norm in front of the projections, the log probabilities behind the last.
 #pragma once
+#include <cstddef>
 #include <cstdint>
 
 #include "rosaq.h"
@@ -21,7 +22,7 @@ struct NormArgs {
 };
 int launch_rmsnorm(const NormArgs& a, void* stream);
 
-constexpr int kMaxTop = 64, kMaxGiven = 4096;
+constexpr int kMaxTop = 64, kMaxGiven = 4096, kMaxParts = 8;
 
 struct LogprobArgs {
   int M, V, type;                                 // ROSAQ_F16, _BF16, _F32
@@ -30,7 +31,13 @@ struct LogprobArgs {
   int given; const int64_t* tokens; float* given_out;
   float* entropy;                                 // null: not wanted
   int top; int64_t* top_ids; float* top_out;
+  int parts; void* ws;                            // workgroups that share a row; more than one, with room for their results
 };
+// Workgroups that would best share a row (at most kMaxParts), and the workspace that they take.
+int parts_of_logprobs(const LogprobArgs& a);
+inline size_t workspace_of_logprobs(const LogprobArgs& a, int parts) {
+  return parts == 1 ? 0 : static_cast<size_t>(a.M) * parts * (16 + 8 * static_cast<size_t>(a.top));
+}
 int launch_logprobs(const LogprobArgs& a, void* stream);
 
 }  // namespace rosaq

@@ -319,26 +319,35 @@ def rmsnorm_codes(x: torch.Tensor, weight: torch.Tensor | None = None, eps: floa
     return codes, scales
 
 
-class LogProbs(NamedTuple):
-    """What logprobs returns; None where nothing was asked for."""
-
+class _LogProbs(NamedTuple):
     given: torch.Tensor | None        # fp32 [M, given]
     entropy: torch.Tensor | None      # fp32 [M]
     top_ids: torch.Tensor | None      # int64 [M, top]
     top: torch.Tensor | None          # fp32 [M, top]
 
 
+class LogProbs(_LogProbs):
+    """What logprobs returns: (given, entropy, top_ids, top), None where nothing was asked for.  Made by logprobs_buffers it has a workspace too."""
+
+    workspace: torch.Tensor | None = None
+
+
 _LOGITS = {torch.float16: B.F16, torch.bfloat16: B.BF16, torch.float32: B.F32}
 
 
 def logprobs_buffers(logits: torch.Tensor, given: int = 0, top: int = 0, entropy: bool = True) -> LogProbs:
-    """Outputs for calls of logprobs over logits of this shape, for loops that keep them."""
-    M, device = logits.shape[0], logits.device
-    real = torch.float32
-    return LogProbs(torch.empty((M, given), dtype=real, device=device) if given else None,
-                    torch.empty(M, dtype=real, device=device) if entropy else None,
-                    torch.empty((M, top), dtype=_INT64, device=device) if top else None,
-                    torch.empty((M, top), dtype=real, device=device) if top else None)
+    """Outputs for calls of logprobs over logits of this shape, for loops that keep them, with a workspace.  Calls with one must not overlap
+    in time."""
+    M, V = logits.shape
+    device, real = logits.device, torch.float32
+    out = LogProbs(torch.empty((M, given), dtype=real, device=device) if given else None,
+                   torch.empty(M, dtype=real, device=device) if entropy else None,
+                   torch.empty((M, top), dtype=_INT64, device=device) if top else None,
+                   torch.empty((M, top), dtype=real, device=device) if top else None)
+    d = B.LogprobsDesc()
+    d.M, d.V, d.type, d.scale, d.top = M, V, _LOGITS[logits.dtype], 1.0, top
+    out.workspace = torch.empty(B.rosaq_workspace_bytes_logprobs(d), dtype=torch.uint8, device=device)
+    return out
 
 
 def logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None, top: int = 0, entropy: bool = True, scale: float = 1.0,
@@ -367,10 +376,12 @@ def logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None, top: int 
         elif t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
             raise ValueError(f"out.{name} must be a contiguous {dtype} tensor {list(shape or ())}")
     d.given_out, d.entropy, d.top_ids, d.top_out = (None if t is None else t.data_ptr() for t in out)
-    device = _device_of(logits, tokens, *out)
+    ws = getattr(out, "workspace", None)          # of a plain tuple there is none: no row is shared then
+    device = _device_of(logits, tokens, ws, *out)
+    at_ws, ws_bytes = (0, 0) if ws is None else (ws.data_ptr(), ws.numel())
     if device != _current_device():
         with torch.cuda.device(device):
-            B.rosaq_logprobs(d, _stream_on(device))
+            B.rosaq_logprobs(d, at_ws, ws_bytes, _stream_on(device))
     else:
-        B.rosaq_logprobs(d, _stream_on(device))
+        B.rosaq_logprobs(d, at_ws, ws_bytes, _stream_on(device))
     return out

@@ -113,7 +113,25 @@ def test_longer_lists_than_there_is_room_for(period, width):
         print(f"case logprobs period {period} {width} {kind}", flush=True)
         x = torch.where(base % period < width, 6.0 + (base * 40503 % 65536) / 65536.0, -2.0 - base % 5)[None].repeat(2, 1)
         x[1] = x[1].flip(0)
-        check(x.to(TYPES[kind]), base[:2].clone(), 64)
+        x = x.to(TYPES[kind])
+        check(x, base[:2].clone(), 64)
+        check(x, base[:2].clone(), 64, out=T.LogProbs(*T.logprobs_buffers(x, given=1, top=64)))
+
+
+@pytest.mark.parametrize("kind", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("M,V,top,given", [(1, 262144, 64, 300), (5, 65537, 20, 1), (64, 70001, 5, 2), (128, 65536, 0, 1), (2, 100003, 64, 0)])
+def test_rows_shared_by_workgroups(M, V, top, given, kind):
+    """With a workspace and without: the same alternatives, the same numbers but for the order of the sums."""
+    print(f"case logprobs shared {M} x {V} {kind} top {top}", flush=True)
+    x = rows(M, V, kind, 3, 1, 1)
+    x[0, V // 2:] = x[0, 0]                   # ties across the parts
+    tokens = torch.randint(-1, V, (M, given), device="cuda") if given else None
+    out = T.logprobs_buffers(x, given=given, top=top)
+    assert out.workspace.numel() > 256
+    out.workspace.fill_(0xff)
+    a = check(x, tokens, top, 0.9, out)
+    b = check(x, tokens, top, 0.9, T.LogProbs(*T.logprobs_buffers(x, given=given, top=top)))
+    assert T.LogProbs(*out).workspace is None and (not top or torch.equal(a.top_ids, b.top_ids))
 
 
 def test_nan_infinities_and_lowest_values():
@@ -132,6 +150,8 @@ def test_nan_infinities_and_lowest_values():
         x[8, 40:90] = np.nan
         tokens = torch.tensor([[4321, 0], [17, 16], [0, 1], [9, 4999], [0, 1], [3, 4000], [0, 1], [0, 4999], [40, 0]], device="cuda")
         got = check(x, tokens, 30)
+        long = torch.cat((x, x, torch.full((9, 70000), -np.inf, dtype=TYPES[kind], device="cuda")), 1)        # in parts
+        check(long, tokens, 30)
         assert bool((got.top_ids[8] == torch.arange(40, 70, device="cuda")).all())
 
 

@@ -59,16 +59,17 @@ def test_rmsnorm_refuses_overlap():
     assert _code(lambda: _norm(ldx=2048, y=X + 1008, ldy=2048)) == ARG and _code(lambda: _norm(ldx=2048, y=X + 2 * 1544, ldy=2048)) == ARG
 
 
-def _logprobs(**over):
+def _logprobs(ws=W, **over):
     d = B.LogprobsDesc()
     for k, v in dict(dict(M=4, V=1000, type=B.F16, scale=1.0, logits=X, ld=1000, given=2, top=5, tokens=Y, given_out=Z, entropy=Z + 0x1000,
                           top_ids=Z + 0x2000, top_out=Z + 0x3000), **over).items():
         setattr(d, k, v)
-    return B.rosaq_logprobs(d)
+    return B.rosaq_logprobs(d, ws)
 
 
 def test_logprobs_refusals():
-    assert B.lib().rosaq_logprobs(None, None) == NULL
+    assert B.lib().rosaq_logprobs(None, W, 0, None) == NULL
+    assert _code(lambda: _logprobs(ws=W + 128)) == ALIGN
     for name in ("logits", "tokens", "given_out", "top_ids", "top_out"):
         assert _code(lambda: _logprobs(**{name: 0})) == NULL, name
     assert _code(lambda: _logprobs(given=0, top=0, entropy=0)) == NULL
@@ -89,3 +90,23 @@ def test_logprobs_refusals():
     for over in (dict(entropy=X + 7996), dict(given_out=Y + 60), dict(top_ids=X - 8), dict(top_ids=Z + 24), dict(top_out=Z + 0x1008),
                  dict(top_out=Z + 0x2000 + 156)):
         assert _code(lambda: _logprobs(**over)) == ARG, over
+
+
+def _logprobs_workspace(M, V, top=5, **over):
+    d = B.LogprobsDesc()
+    for k, v in dict(dict(M=M, V=V, top=top, scale=1.0), **over).items():
+        setattr(d, k, v)
+    return B.rosaq_workspace_bytes_logprobs(d)
+
+
+def test_logprobs_workspace():
+    assert _logprobs_workspace(4096, 32000) == 256 and _logprobs_workspace(1, 1000) == 256
+    for over in (dict(M=0), dict(V=0), dict(type=5), dict(top=65), dict(scale=0.0)):
+        with pytest.raises(B.RosaqError):
+            _logprobs_workspace(**dict(dict(M=1, V=1000), **over))
+    # 16 bytes of sums and 8 an alternative for every part, of which there are at most 8
+    for M, V, top in ((1, 262144, 64), (3, 131071, 5), (8, 100000, 0), (1, 1 << 30, 20)):
+        n = _logprobs_workspace(M, V, top)
+        part = M * (16 + 8 * top)
+        assert n == 256 or (n % part == 0 and 2 <= n // part <= 8)
+    assert _logprobs_workspace(1, 262144, 64) > 256
