@@ -74,7 +74,7 @@ def test_parts_hold_all_steps(group, max_rows, window, sinks):
             start = 0 if sinks >= start else start
             most = max(most, over + -(-max(n - max_rows + last + 1 - start, 0) // step))
     assert most <= bound
-    parts = min(max((2048 if few else 512) // tiles, 1), max(1, bound // (8 if few else 2)))
+    parts = min(max((768 if few else 512) // tiles, 1), max(1, bound // (8 if few else 2)))
     steps = -(-bound // parts)
     assert _parts(window, sinks, 1, group, max_rows, 1, max_rows, max_kv) == -(-bound // steps)
 
