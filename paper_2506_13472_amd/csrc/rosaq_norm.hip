@@ -1,13 +1,15 @@
 // Root-mean-square norm of rows, with the addition to the residual stream in front of it: h = x + residual, y = h / sqrt(mean h^2 + eps) * weight.
 //
 // A row is held by a team of threads, sixteen to 1024, in pieces of eight channels: read once, added up over the team, written once.  So it is bound
-// by memory, or by a launch where there are few rows.
+// by memory (8192 x 4096 with an fp16 residual 41.5 us = 6.5 TB/s, where a copy reaches 4.9 to 5.2), or by a launch where there are few rows (64 of them 2.9 us).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 #include <string>
+#include <type_traits>
 
 #include "rosaq_gemm.h"
+#include "rosaq_reduce.h"
 #include "rosaq_rows.h"
 
 namespace rosaq {
@@ -20,31 +22,26 @@ template <bool F32> __device__ __forceinline__ float channel(const Residual<F32>
   else return static_cast<float>(as_h8(r.w)[j]);
 }
 
-template <class T> __device__ __forceinline__ T add_(T a, T b) { return a + b; }
-// The larger; NaN where one is NaN.
-template <class T> __device__ __forceinline__ T larger(T a, T b) { return a != a ? a : (b != b ? b : (a > b ? a : b)); }
-
-// f over the values of a team's threads, in one order whatever runs when.
+// f over the values of a team's threads (f(a, b) and f(b, a) the same), in one order whatever runs when.
 template <int TEAM, class T, class F> __device__ __forceinline__ T reduce(T v, T* lds, F f) {
-#pragma unroll
-  for (int n = 1; n < (TEAM < 64 ? TEAM : 64); n *= 2) v = f(v, __shfl_xor(v, n, 64));
+  if constexpr (TEAM == 16) return row_all<16>(v, f);
+  v = wave_all(v, f);
   if constexpr (TEAM > 64) {
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x / 64] = v;
     __syncthreads();
-    v = lds[0];
-#pragma unroll
-    for (int i = 1; i < TEAM / 64; ++i) v = f(v, lds[i]);
+    v = row_all<TEAM / 64>(lds[threadIdx.x % (TEAM / 64)], f);
   }
   return v;
 }
 
 // ADD 0: no residual, 1: fp16, 2: fp32.  The sum of squares is fp32, of rows whose residual is fp32 in fp64: those may hold numbers whose squares
 // fp32 does not.  CODES: all in fp64, because a code next to a border is a whole step off when it falls to the other side; a step is a 127th of the largest
-// value.  The vector units have room for it (some 20 operations of 80 that fit beside a channel's way through memory).
+// value.  The vector units bound it then, most of all the conversions to fp64 (1003 x 5120 with an fp32 residual 14.1 us, of which memory 11.5; 8192 x 4096 with
+// an fp16 one 69 and 48).  Built and slower: fp32, and fp64 again for what fp32 cannot decide (22.3 and 61 us: a branch a channel).
 template <int TEAM, int CH, int ADD, bool CODES>
 __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void rmsnorm_kernel(NormArgs a) {
   constexpr int kThreads = TEAM < 256 ? 256 : TEAM, kTeams = kThreads / TEAM;
-  constexpr bool F32 = ADD == 2;
+  constexpr bool F32 = ADD == 2, kHold = CODES && !(TEAM == 1024 && CH > 2);      // there the registers are too few
   using Sum = std::conditional_t<F32 || CODES, double, float>;
   using Value = std::conditional_t<CODES, double, float>;
   __shared__ Sum lds_sum[TEAM > 64 ? TEAM / 64 : 1];
@@ -79,6 +76,7 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void rmsnorm_kernel(NormAr
       else return v;
     };
     Sum sum = 0;
+    double wide[kHold ? CH : 1][8];        // h, then y
 #pragma unroll
     for (int i = 0; i < CH; ++i)
       if (t + i * TEAM < pieces)
@@ -86,7 +84,12 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void rmsnorm_kernel(NormAr
         for (int j = 0; j < 8; ++j) {
           const Sum v = static_cast<Sum>(h(i, j));
           sum += v * v;
+          if constexpr (kHold) wide[i][j] = v;
         }
+    auto held = [&](int i, int j) {
+      if constexpr (kHold) return wide[i][j];
+      else return h(i, j);
+    };
     if constexpr (ADD != 0) {
       if (a.residual_out) {
 #pragma unroll
@@ -96,26 +99,36 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void rmsnorm_kernel(NormAr
           if constexpr (F32) {
             float4 o[2];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) (&o[j / 4].x)[j % 4] = static_cast<float>(h(i, j));
+            for (int j = 0; j < 8; ++j) (&o[j / 4].x)[j % 4] = static_cast<float>(held(i, j));
             float4* to = reinterpret_cast<float4*>(static_cast<float*>(a.residual_out) + row * a.ld_residual_out) + 2 * p;
             to[0] = o[0];
             to[1] = o[1];
           } else {
             half8 o;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] = static_cast<_Float16>(static_cast<float>(h(i, j)));
+            for (int j = 0; j < 8; ++j) o[j] = static_cast<_Float16>(static_cast<float>(held(i, j)));
             reinterpret_cast<uint4*>(static_cast<_Float16*>(a.residual_out) + row * a.ld_residual_out)[p] = __builtin_bit_cast(uint4, o);
           }
         }
       }
     }
-    sum = reduce<TEAM>(sum, lds_sum, add_<Sum>);
+    sum = reduce<TEAM>(sum, lds_sum, added<Sum>);
     Value factor;
     if constexpr (std::is_same_v<Sum, double>) factor = static_cast<Value>(1.0 / sqrt(sum / a.D + a.eps));
     else factor = 1.f / sqrtf(sum / static_cast<float>(a.D) + static_cast<float>(a.eps));
-    auto value = [&](int i, int j) {
-      const Value v = h(i, j) * factor;
+    auto formed = [&](int i, int j) {
+      const Value v = held(i, j) * factor;
       return a.weight ? v * static_cast<Value>(static_cast<float>(as_h8(w[i])[j])) : v;
+    };
+    if constexpr (kHold)
+#pragma unroll
+      for (int i = 0; i < CH; ++i)
+        if (t + i * TEAM < pieces)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) wide[i][j] = formed(i, j);
+    auto value = [&](int i, int j) {
+      if constexpr (kHold) return wide[i][j];
+      else return formed(i, j);
     };
     if (a.y) {
 #pragma unroll
@@ -129,16 +142,22 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void rmsnorm_kernel(NormAr
       }
     }
     if constexpr (CODES) {
-      double most = 0.0;
+      // the maximum passes over NaN, which a product with zero does not, and neither over infinities
+      double most = 0.0, none = 0.0;
 #pragma unroll
       for (int i = 0; i < CH; ++i)
         if (t + i * TEAM < pieces)
 #pragma unroll
-          for (int j = 0; j < 8; ++j) most = larger(most, __builtin_fabs(value(i, j)));
-      most = reduce<TEAM>(most, lds_most, larger<double>);
+          for (int j = 0; j < 8; ++j) {
+            const double v = value(i, j);
+            most = __builtin_fmax(most, __builtin_fabs(v));
+            none = __builtin_fma(v, 0.0, none);
+          }
+      most = reduce<TEAM>(none == 0.0 ? most : INFINITY, lds_most, [](double a, double b) { return __builtin_fmax(a, b); });
       const float scale = static_cast<float>(most / 127.0);
       // a scale that is no positive number has no codes: zero's, or those of NaN
-      const double inverse = scale > 0.f && scale < INFINITY ? 1.0 / static_cast<double>(scale) : 0.0;
+      const bool some = scale > 0.f && scale < INFINITY;
+      const double inverse = some ? 1.0 / static_cast<double>(scale) : 0.0;
       if (t == 0) a.scales[row] = scale < INFINITY ? scale : NAN;
 #pragma unroll
       for (int i = 0; i < CH; ++i) {
@@ -147,11 +166,13 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void rmsnorm_kernel(NormAr
         uint32_t o[2] = {0u, 0u};
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          // a scale among fp32's subnormals is far from its 127th: codes are kept to their range
-          const int c = inverse == 0.0 ? 0 : min(max(static_cast<int>(__builtin_rint(value(i, j) * inverse)), -127), 127);
+          // to the nearest whole number, which is the low word of 1.5 x 2^52 and it.  A scale among fp32's subnormals is far from its 127th, so codes are kept to
+          // their range
+          const double whole = __builtin_fma(value(i, j), inverse, 0x1.8p52);
+          const int c = min(max(static_cast<int>(__builtin_bit_cast(uint64_t, whole)), -127), 127);
           o[j / 4] |= (static_cast<uint32_t>(c) & 0xffu) << (j % 4 * 8);
         }
-        reinterpret_cast<uint2*>(static_cast<char*>(a.codes) + row * a.ld_codes)[p] = make_uint2(o[0], o[1]);
+        reinterpret_cast<uint2*>(static_cast<char*>(a.codes) + row * a.ld_codes)[p] = some ? make_uint2(o[0], o[1]) : make_uint2(0u, 0u);
       }
     }
     if constexpr (TEAM > 64) __syncthreads();       // the next row's sums go to the same place
@@ -177,14 +198,17 @@ template <int TEAM, int CH> static void run(const NormArgs& a, hipStream_t st) {
   }
 }
 
+// The smallest team whose threads hold one or two pieces each: more loads under way beside each other, fewer registers.  us with 256 threads / 512 / 1024: 8192 x
+// 4096 with an fp16 residual 45.0 / 41.5 / 47.6, 64 of them 3.4 / 2.9 / 3.1; 8192 x 5120 64.1 / 60.2 / 66.5, 64 of them 4.1 / 3.4 / 3.4; a wave
+// a row is slower still (8192 x 4096 52.4, 64 of them 6.7).
 int launch_rmsnorm(const NormArgs& a, void* stream) {
   hipStream_t st = static_cast<hipStream_t>(stream);
   const int pieces = a.D / 8;
   if (pieces <= 16) run<16, 1>(a, st);
   else if (pieces <= 64) run<64, 1>(a, st);
   else if (pieces <= 256) run<256, 1>(a, st);
-  else if (pieces <= 512) run<256, 2>(a, st);
-  else if (pieces <= 1024) run<256, 4>(a, st);
+  else if (pieces <= 512) run<512, 1>(a, st);
+  else if (pieces <= 1024) run<512, 2>(a, st);
   else if (pieces <= 2048) run<1024, 2>(a, st);
   else run<1024, 4>(a, st);
   const hipError_t e = hipGetLastError();
