@@ -231,14 +231,18 @@ def shape_sweep(torch, shapes, ms_override, reps, emit):
         del W16, w16
 
 
-def decode_layer(B, T, lay, qkv, x, heads, xh, gated, y, ws, chained_mlp, attend=None):
+def decode_layer(B, T, lay, qkv, x, heads, xh, gated, y, ws, chained_mlp, attend=None, norm=None):
     """The linears of one layer on the current stream: q/k/v of x into the buffers of `qkv`, o of `heads`, the FFN of x.  `attend` is called
-    between q/k/v and o, to make `heads`; the rest is the same with and without it."""
+    between q/k/v and o, to make `heads`, `norm` in front of q/k/v and of the FFN, to make x from y; the rest is the same with and without them."""
     M, sp = x.shape[0], T.current_stream_ptr()
+    if norm is not None:
+        norm()
     B.rosaq_linear_batch(qkv, x.data_ptr(), M, x.stride(0), ws.data_ptr(), ws.numel(), sp)
     if attend is not None:
         attend()
     T.linear(lay["o"], heads, y, ws)
+    if norm is not None:
+        norm()
     if chained_mlp:
         # gate and up in one launch, silu(gate) * up applied in its epilogue and written as the
         # down projection's input fragments; then the down projection
@@ -250,7 +254,7 @@ def decode_layer(B, T, lay, qkv, x, heads, xh, gated, y, ws, chained_mlp, attend
         T.linear(lay["down"], xh, y, ws)
 
 
-def decode_workload(torch, steps, warmup, absorbed=False, chained_mlp=True, context=0, cache_bits=4):
+def decode_workload(torch, steps, warmup, absorbed=False, chained_mlp=True, context=0, cache_bits=4, window=0, sinks=0, whole=False):
     """The linears of a LLaMA-7B-shaped decode step at batch 64, INT4 g128, K = 128: per layer
     q/k/v (one batched call, shared head-wise rotation), o (head-wise), gate/up (one batched call
     sharing one dense 4096 x 4096 rotation) and down (no rotation, the paper's setting for W_D);
@@ -260,7 +264,9 @@ def decode_workload(torch, steps, warmup, absorbed=False, chained_mlp=True, cont
     of the same shape.  Returns a dict with the time per step next to the same linears as fp16
     torch.matmul calls.  With `context` tokens per sequence the step is also timed with what lies between
     q/k/v and o: rotary positions and the new tokens' keys and values to a cache of `cache_bits` bits
-    (rosaq_cache_append), attention over the cache (rosaq_attention), every layer its own cache."""
+    (rosaq_cache_append), attention over the cache (rosaq_attention; with `window` rosaq_attention_window over so many tokens and the first `sinks`),
+    every layer its own cache.  With `whole` also with all that is left of the step: the residual stream in fp32 and its norms (rosaq_rmsnorm), the
+    projection to 32000 logits and their log probabilities with five alternatives (rosaq_logprobs)."""
     from paper_2506_13472_amd import binding as B, synth, torch_glue as T
     dev = torch.device("cuda:0")
     timer = Timer(torch, torch.cuda.Stream())
@@ -301,19 +307,30 @@ def decode_workload(torch, steps, warmup, absorbed=False, chained_mlp=True, cont
         for l, lay in enumerate(layers):
             decode_layer(B, T, lay, qkv[l], x, x, xh, y_f[0], y_d[3], ws, chained_mlp)
 
-    def step_with_attention():
+    def step_with_attention(x=x, norm=None):
         def attend(l):
             T.cache_append(caches[l], slots, y_d[1], y_d[2], rope=rope, positions=positions, q=y_d[0], q_out=y_d[0])
             T.attention(plans[l], y_d[0], lengths, pages, out=y_att)
 
         for l, lay in enumerate(layers):
-            decode_layer(B, T, lay, qkv[l], x, y_att, xh, y_f[0], y_d[3], ws, chained_mlp, functools.partial(attend, l))
+            decode_layer(B, T, lay, qkv[l], x, y_att, xh, y_f[0], y_d[3], ws, chained_mlp, functools.partial(attend, l), norm)
+
+    def whole_step():
+        def norm():
+            T.rmsnorm(y_d[3], norm_weight, residual=stream, out=x_normed)
+
+        stream.copy_(embedded)
+        y_d[3].zero_()
+        step_with_attention(x_normed, norm)
+        norm()
+        T.linear(head, x_normed, logits, ws_head)
+        T.logprobs(logits, top=5, out=log_probs)
 
     if context:
         page = 64
         per_seq = -(-context // page)
         caches = [T.KvCache(d // 128, 128, cache_bits, page, M * per_seq) for _ in range(L)]
-        plans = [T.AttentionPlan(c, d // 128, M, max_kv=context) for c in caches]
+        plans = [T.AttentionPlan(c, d // 128, M, max_kv=context, window=window or None, sinks=sinks) for c in caches]
         rope = T.Rope(T.rope_table(context, 128))
         pages = torch.randperm(M * per_seq, device=dev).to(torch.int32).view(M, per_seq)
         lengths = torch.full((M,), context, dtype=torch.int32, device=dev)
@@ -325,6 +342,13 @@ def decode_workload(torch, steps, warmup, absorbed=False, chained_mlp=True, cont
             kv = [torch.randn((M * context, d), device=dev).to(torch.float16) for _ in range(2)]
             T.cache_append(c, every.flatten(), *kv)
         del kv
+    if whole:
+        head = B.rosaq_pack_weights(synth.make_weight(47, 32000, d), None, synth.descending_spectrum(27, d, 1), K, 4, B.Q_NONE)
+        ws_head = T.alloc_workspace(head, M)
+        embedded, norm_weight = torch.randn((M, d), device=dev), torch.ones(d, dtype=torch.float16, device=dev)
+        stream, x_normed = embedded.clone(), torch.empty_like(x)
+        logits = torch.empty((M, 32000), dtype=torch.float16, device=dev)
+        log_probs = T.logprobs_buffers(logits, top=5)
 
     # fp16: the same seven linears per layer as separate vendor GEMMs, and with q/k/v and gate/up fused
     W_qkv = [torch.randn((3 * d, d), dtype=torch.float16, device=dev) * 0.02 for _ in range(L)]
@@ -355,6 +379,7 @@ def decode_workload(torch, steps, warmup, absorbed=False, chained_mlp=True, cont
     t_gemm = timer.run(step, steps, warmup)
     B.rosaq_tune("stages", 3)
     t_att = timer.run(step_with_attention, steps, warmup) if context else None
+    t_whole = timer.run(whole_step, steps, warmup) if whole else None
     t16f = timer.run(step16_fused, steps, warmup)
     t16s = timer.run(step16_separate, steps, warmup)
 
@@ -390,13 +415,19 @@ def decode_workload(torch, steps, warmup, absorbed=False, chained_mlp=True, cont
         "speedup_vs_fp16_separate": round(t16s["median"] / ms, 3),
         "data": "synthetic"}
     if context:
-        cache_bytes = 2 * M * context * (d // 128) * (16 * cache_bits + 4)
+        seen = min(context, window + sinks) if window else context
+        cache_bytes = 2 * M * seen * (d // 128) * (16 * cache_bits + 4)
         extra = t_att["median"] - ms
         out["with_attention"] = {
-            "context": context, "cache_bits": cache_bits, "ms_per_step": round(t_att["median"], 4),
+            "context": context, **({"window": window, "sinks": sinks} if window else {}), "cache_bits": cache_bits, "ms_per_step": round(t_att["median"], 4),
             "tokens_per_s": round(M / (t_att["median"] * 1e-3), 1), "attention_ms_per_step": round(extra, 4),
             "cache_GB_read_per_step": round(cache_bytes * L / 1e9, 3),
             "attention_GBps": round(cache_bytes * L / extra / 1e6, 1)}
+    if whole:
+        out["whole_step"] = {
+            "adds": "2 x 32 + 1 rosaq_rmsnorm (fp32 stream), rosaq_linear to 32000 logits, rosaq_logprobs with 5 alternatives",
+            "ms_per_step": round(t_whole["median"], 4), "tokens_per_s": round(M / (t_whole["median"] * 1e-3), 1)}
+        head.free()
     for lay in layers:
         for h in lay.values():
             h.free()
@@ -433,6 +464,11 @@ def main():
     ap.add_argument("--attention", type=int, default=0, metavar="TOKENS",
                     help="with --decode: also time the step with rotary positions, a quantised cache and attention over "
                          "this many tokens per sequence between the q/k/v and output projections")
+    ap.add_argument("--window", type=int, default=0, metavar="TOKENS",
+                    help="with --attention: every row looks back this many tokens only")
+    ap.add_argument("--sinks", type=int, default=0, metavar="TOKENS", help="with --window: and to the first so many")
+    ap.add_argument("--whole-step", action="store_true",
+                    help="with --attention: also time the step with norms, head projection and log probabilities")
     ap.add_argument("--cache-bits", type=int, default=4, choices=[4, 8], help="with --attention: bits of the cache")
     ap.add_argument("--sweep-filter", default="", help="substring of the shape names to run")
     ap.add_argument("--sweep-m", default="", help="comma-separated M values replacing each shape's own list")
@@ -478,9 +514,11 @@ def main():
         ms = [int(v) for v in args.sweep_m.split(",")] if args.sweep_m else None
         shape_sweep(torch, shapes, ms, 20, lambda row: print(json.dumps(row), flush=True))
         return
+    if (args.window and not args.attention) or (args.whole_step and not args.attention) or (args.sinks and not args.window):
+        ap.error("--window and --whole-step go with --attention, --sinks with --window")
     if args.decode:
         print(json.dumps(decode_workload(torch, args.decode_steps, args.warmup, args.absorbed, not args.unchained_mlp,
-                                         args.attention, args.cache_bits)), flush=True)
+                                         args.attention, args.cache_bits, args.window, args.sinks, args.whole_step)), flush=True)
         return
 
     # ---- synthetic layers: calibrate (PCA per head on the GPU), pack, all through the C ABI ------

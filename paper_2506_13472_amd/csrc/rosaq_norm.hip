@@ -113,11 +113,16 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void rmsnorm_kernel(NormAr
       }
     }
     sum = reduce<TEAM>(sum, lds_sum, added<Sum>);
+    // of rows whose residual is fp32 the factor may be beyond fp32, and its power of two goes to h first
     Value factor;
-    if constexpr (std::is_same_v<Sum, double>) factor = static_cast<Value>(1.0 / sqrt(sum / a.D + a.eps));
+    int power = 0;
+    if constexpr (CODES) factor = 1.0 / sqrt(sum / a.D + a.eps);
+    else if constexpr (F32) factor = static_cast<float>(frexp(1.0 / sqrt(sum / a.D + a.eps), &power));
     else factor = 1.f / sqrtf(sum / static_cast<float>(a.D) + static_cast<float>(a.eps));
     auto formed = [&](int i, int j) {
-      const Value v = held(i, j) * factor;
+      Value v = held(i, j);
+      if constexpr (F32 && !CODES) v = __builtin_ldexpf(v, power);
+      v *= factor;
       return a.weight ? v * static_cast<Value>(static_cast<float>(as_h8(w[i])[j])) : v;
     };
     if constexpr (kHold)
