@@ -10,6 +10,8 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "rosaq_attention.h"
 #include "rosaq_gemm.h"
 
@@ -49,14 +51,14 @@ __device__ __forceinline__ int steps_of(const AttendArgs& a, int over, int step,
   return prefix_steps_of(a, over, step) + (over == kPrefix ? 0 : (visible(a, tokens, count, i) + step - 1) / step);
 }
 
-// With a window (W) row i, at position p = tokens - count + i, sees token j <= p if j > p - window or j < sinks.  A tile's steps then go over the sinks,
-// where a gap lies behind them, and from the whole step that the first row's window begins in to the last row.  Tokens that no row of the tile
+// With a window (W) row i, at position p = tokens - count + i, sees token j <= p if j > p - window or j < sinks.  A tile's steps then go from the whole step
+// that the first row's window begins in to the last row, and then over the sinks, where a gap lies behind them.  Tokens that no row of the tile
 // sees are neither counted on to be in the cache nor their pages to be the sequence's: of those that lie in the same step nothing is used.
 __device__ __forceinline__ int lowest(const AttendArgs& a, int tokens, int count, int i) { return max(tokens - count + i + 1 - a.window, 0); }
 struct Walk {
-  int over_sinks = 0;      // steps
-  int start = 0;           // token that the steps behind those begin with
+  int start = 0;           // token that the steps begin with
   int low = 0;             // token that the first row's window begins with
+  int to_sinks = 0;        // steps in front of those over the sinks
   int all = 0;             // steps
 };
 __device__ __forceinline__ Walk walk_of(const AttendArgs& a, int step, int tokens, int count, int first, int last) {
@@ -64,12 +66,12 @@ __device__ __forceinline__ Walk walk_of(const AttendArgs& a, int step, int token
   w.low = lowest(a, tokens, count, first);
   w.start = w.low / step * step;
   if (a.sinks >= w.start) w.start = 0;
-  else w.over_sinks = (a.sinks + step - 1) / step;
-  w.all = w.over_sinks + (max(visible(a, tokens, count, last) - w.start, 0) + step - 1) / step;
+  w.to_sinks = (max(visible(a, tokens, count, last) - w.start, 0) + step - 1) / step;
+  w.all = w.to_sinks + (w.start ? (a.sinks + step - 1) / step : 0);
   return w;
 }
 __device__ __forceinline__ int token_of(const Walk& w, int step, int tokens) {
-  return step < w.over_sinks ? step * tokens : w.start + (step - w.over_sinks) * tokens;
+  return step < w.to_sinks ? w.start + step * tokens : (step - w.to_sinks) * tokens;
 }
 
 // A workgroup's share of a launch.  Workgroups go to the XCDs in turn; with by_xcd, those of one sequence and kv head, which read
@@ -267,7 +269,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const AttendLau
   // pages of a step, given how many tokens the sequence has
   auto pages_of = [&](int step, int tokens) {
     if constexpr (W) {
-      const int held = step < walk.over_sinks ? min(a.sinks, tokens) : tokens;
+      const int held = step < walk.to_sinks ? tokens : min(a.sinks, tokens);
       return look_up<2>(own_pages, token_of(walk, step, kStep) / kCacheBlock, (held + kCacheBlock - 1) / kCacheBlock, block_shift);
     }
     const bool own = step >= prefix_steps;
@@ -579,7 +581,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
 
   auto pages_of = [&](int stage) {
     if constexpr (W) {
-      const int held = stage < walk.over_sinks ? min(a.sinks, tokens) : tokens;
+      const int held = stage < walk.to_sinks ? tokens : min(a.sinks, tokens);
       return look_up<4>(own_pages, token_of(walk, stage, kStage) / kCacheBlock, stage < end ? (held + kCacheBlock - 1) / kCacheBlock : 0, block_shift);
     }
     const bool own = stage >= prefix_stages;
@@ -691,7 +693,9 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
     for (int j = 0; j < U; ++j) sum[t][j] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
 
-  auto multiply = [&](int stage, int hidden, const StageLds<D>& from) {
+  // NB: records of the stage that count
+  auto multiply = [&](auto records, int stage, int hidden, const StageLds<D>& from) {
+    constexpr int NB = decltype(records)::value;
     const bool own = W || stage >= prefix_stages;
     const int t0 = W ? token_of(walk, stage, kStage) : (own ? stage - prefix_stages : stage) * kStage;
     if (own && t0 >= most_seen) return;
@@ -703,17 +707,17 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
     for (int t = 0; t < RT; ++t) base[t] = ref[t] == kNoScore ? 0.f : ref[t];
     floatx4 start[4];
 #pragma unroll
-    for (int b = 0; b < 4; ++b) start[b] = *reinterpret_cast<const floatx4*>(&from.start[b * kCacheBlock + 4 * g]);
+    for (int b = 0; b < NB; ++b) start[b] = *reinterpret_cast<const floatx4*>(&from.start[b * kCacheBlock + 4 * g]);
 #pragma unroll
     for (int s = 0; s < KS; ++s)         // a product never waits for the sum of the one before
 #pragma unroll
-      for (int b = 0; b < 4; ++b) {
+      for (int b = 0; b < NB; ++b) {
         const half8 f = as_h8(from.k[b][s][lane]);
 #pragma unroll
         for (int t = 0; t < RT; ++t) score[b][t] = mfma16(f, q[t][s], s ? score[b][t] : start[b]);
       }
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
+    for (int b = 0; b < NB; ++b) {
       const floatx4 scale = *reinterpret_cast<const floatx4*>(&from.scale[b * kCacheBlock + 4 * g]);
 #pragma unroll
       for (int t = 0; t < RT; ++t)
@@ -722,7 +726,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
     }
     if (masked) {
 #pragma unroll
-      for (int b = 0; b < 4; ++b)
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
           const int lim = (own ? limit[t] : a.prefix_len) - t0 - b * kCacheBlock - 4 * g;
@@ -739,7 +743,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
     for (int t = 0; t < RT; ++t) {
       most[t] = score[0][t][0];
 #pragma unroll
-      for (int i = 1; i < 16; ++i) most[t] = fmaxf(most[t], score[i / 4][t][i % 4]);
+      for (int i = 1; i < 4 * NB; ++i) most[t] = fmaxf(most[t], score[i / 4][t][i % 4]);
       over |= most[t] > (ref[t] == kNoScore ? kNoScore : kRoom);
     }
     if (__any(over)) {
@@ -754,12 +758,12 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
 #pragma unroll
         for (int j = 0; j < U; ++j) sum[t][j] *= floatx4{down, down, down, down};
 #pragma unroll
-        for (int i = 0; i < 16; ++i) score[i / 4][t][i % 4] -= up;
+        for (int i = 0; i < 4 * NB; ++i) score[i / 4][t][i % 4] -= up;
         ref[t] = base[t] + up;
       }
     }
 #pragma unroll
-    for (int p = 0; p < 2; ++p) {
+    for (int p = 0; p < (NB + 1) / 2; ++p) {
       half8 prob[RT];
       floatx4 inverse[2];
 #pragma unroll
@@ -768,6 +772,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
       for (int t = 0; t < RT; ++t)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
+          if (2 * p + i / 4 >= NB) { prob[t][i] = static_cast<_Float16>(0.f); continue; }
           const float e = __builtin_amdgcn_exp2f(score[2 * p + i / 4][t][i % 4]);
           l[t] = __builtin_fmaf(e, inverse[i / 4][i % 4], l[t]);
           prob[t][i] = static_cast<_Float16>(e);
@@ -781,6 +786,8 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
     }
   };
 
+  // few sinks are one record, which takes a third of a stage's products
+  const int short_one = W && end > begin && end > walk.to_sinks && a.sinks <= kCacheBlock ? 1 : 0;
   if (begin < end) {
     Codes x;
     int hidden;
@@ -790,17 +797,18 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
     store(begin, x, lds[0]);
     hidden = x.hidden;
     lds_barrier();
-    for (int stage = begin, cur = 0; stage < end; ++stage, cur ^= 1) {
+    for (int stage = begin, cur = 0; stage < end - short_one; ++stage, cur ^= 1) {
       if (stage + 1 < end) {
         load(stage + 1, next, x);
         next = pages_of(stage + 2);
       }
-      if (!idle) multiply(stage, hidden, lds[kBuffers == 1 ? 0 : cur]);
+      if (!idle) multiply(std::integral_constant<int, 4>{}, stage, hidden, lds[kBuffers == 1 ? 0 : cur]);
       if (kBuffers == 1) lds_barrier();
       if (stage + 1 < end) store(stage + 1, x, lds[kBuffers == 1 ? 0 : cur ^ 1]);
       hidden = x.hidden;
       lds_barrier();
     }
+    if (W && short_one && !idle) multiply(std::integral_constant<int, 1>{}, end - 1, hidden, lds[kBuffers == 1 ? 0 : (end - 1 - begin) & 1]);
   }
 
   const Part<D> out(a, parts);
