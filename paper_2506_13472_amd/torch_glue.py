@@ -263,33 +263,48 @@ def _row_stride(name: str, x: torch.Tensor, rows: int, width: int, dtype: torch.
     return stride[0] if rows > 1 else width
 
 
+def _beside(name: str, t: torch.Tensor, shape: torch.Size, dtype: torch.dtype, device: int) -> int:
+    """The row stride of a matrix of a call whose first one is of this shape and device (_row_stride and _device_of in one look)."""
+    if t.dtype is not dtype or t.shape != shape:
+        raise ValueError(f"{name} must be a {dtype} tensor {list(shape)} with unit column stride")
+    if t.get_device() != device:
+        raise ValueError("the tensors of a call must lie on one GPU")
+    return shape[1] if t.is_contiguous() else _row_stride(name, t, shape[0], shape[1], dtype)
+
+
 def _rmsnorm(x, weight, eps, residual, residual_out, y, codes, scales):
     """One rosaq_rmsnorm call on x's device; y, codes and scales: None, or where they go."""
-    M, D = x.shape
+    shape, device = x.shape, x.get_device()
+    M, D = shape
     d = B.RmsNormDesc()
     d.M, d.D, d.eps = M, D, eps
-    d.x, d.ldx = x.data_ptr(), _ld("x", x, M, D)
+    d.ldx, d.x = _beside("x", x, shape, _HALF, device), x.data_ptr()
+    if device < 0:
+        raise ValueError("the tensors of a call must lie on a GPU")
     if weight is not None:
-        if weight.dtype is not _HALF or weight.shape != (D,) or not weight.is_contiguous():
-            raise ValueError(f"weight must be a contiguous fp16 tensor [{D}]")
+        if weight.dtype is not _HALF or weight.shape != shape[1:] or not weight.is_contiguous() or weight.get_device() != device:
+            raise ValueError(f"weight must be a contiguous fp16 tensor [{D}] on x's GPU")
         d.weight = weight.data_ptr()
     if residual is not None:
         dtype = residual.dtype
-        if dtype is not _HALF and dtype is not torch.float32:
+        if dtype is torch.float32:
+            d.residual_type = B.F32
+        elif dtype is not _HALF:
             raise ValueError("residual must be fp16 or fp32")
-        d.residual_type = B.F16 if dtype is _HALF else B.F32
-        d.residual, d.ld_residual = residual.data_ptr(), _row_stride("residual", residual, M, D, dtype)
-        d.residual_out, d.ld_residual_out = residual_out.data_ptr(), _row_stride("residual_out", residual_out, M, D, dtype)
+        d.ld_residual, d.residual = _beside("residual", residual, shape, dtype, device), residual.data_ptr()
+        if residual_out is None or residual_out is residual:
+            d.ld_residual_out, d.residual_out = d.ld_residual, d.residual
+        else:
+            d.ld_residual_out, d.residual_out = _beside("residual_out", residual_out, shape, dtype, device), residual_out.data_ptr()
     elif residual_out is not None:
         raise ValueError("residual_out without a residual")
     if y is not None:
-        d.y, d.ldy = y.data_ptr(), _ld("out", y, M, D)
+        d.ldy, d.y = _beside("out", y, shape, _HALF, device), y.data_ptr()
     if codes is not None:
-        d.codes, d.ld_codes = codes.data_ptr(), _row_stride("codes", codes, M, D, torch.int8)
-        if scales.dtype is not torch.float32 or scales.shape != (M,) or not scales.is_contiguous():
-            raise ValueError(f"scales must be a contiguous fp32 tensor [{M}]")
+        d.ld_codes, d.codes = _beside("codes", codes, shape, torch.int8, device), codes.data_ptr()
+        if scales.dtype is not torch.float32 or scales.shape != shape[:1] or not scales.is_contiguous() or scales.get_device() != device:
+            raise ValueError(f"scales must be a contiguous fp32 tensor [{M}] on x's GPU")
         d.scales = scales.data_ptr()
-    device = _device_of(x, weight, residual, residual_out, y, codes, scales)
     if device != _current_device():
         with torch.cuda.device(device):
             B.rosaq_rmsnorm(d, _stream_on(device))
@@ -302,7 +317,7 @@ def rmsnorm(x: torch.Tensor, weight: torch.Tensor | None = None, eps: float = 1e
     """rosaq_rmsnorm of x [M, D] + residual (fp16 or fp32): fp16 [M, D].  The sum goes to residual_out, which is residual itself
     unless given; out may be x or residual where the sum does not go there."""
     y = torch.empty(x.shape, dtype=_HALF, device=x.device) if out is None else out
-    _rmsnorm(x, weight, eps, residual, residual if residual_out is None else residual_out, y, None, None)
+    _rmsnorm(x, weight, eps, residual, residual_out, y, None, None)
     return y
 
 
@@ -315,7 +330,7 @@ def rmsnorm_codes(x: torch.Tensor, weight: torch.Tensor | None = None, eps: floa
         codes = torch.empty((M, D), dtype=torch.int8, device=x.device)
     if scales is None:
         scales = torch.empty(M, dtype=torch.float32, device=x.device)
-    _rmsnorm(x, weight, eps, residual, residual if residual_out is None else residual_out, out, codes, scales)
+    _rmsnorm(x, weight, eps, residual, residual_out, out, codes, scales)
     return codes, scales
 
 
@@ -354,12 +369,16 @@ def logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None, top: int 
              out: LogProbs | None = None) -> LogProbs:
     """rosaq_logprobs of logits [M, V] (fp16, bf16 or fp32): of tokens int64 [M, given], or [M] for one of each row (below zero: padding), and
     of the `top` largest, with the entropy.  out (logprobs_buffers) says instead of `entropy` whether that is wanted."""
-    M, V = logits.shape
-    if logits.dtype not in _LOGITS:
+    shape, device = logits.shape, logits.get_device()
+    M, V = shape
+    kind = _LOGITS.get(logits.dtype)
+    if kind is None:
         raise ValueError("logits must be fp16, bf16 or fp32")
     d = B.LogprobsDesc()
-    d.M, d.V, d.type, d.scale, d.top = M, V, _LOGITS[logits.dtype], scale, top
-    d.logits, d.ld = logits.data_ptr(), _row_stride("logits", logits, M, V, logits.dtype)
+    d.M, d.V, d.type, d.scale, d.top = M, V, kind, scale, top
+    d.ld, d.logits = _beside("logits", logits, shape, logits.dtype, device), logits.data_ptr()
+    if device < 0:
+        raise ValueError("the tensors of a call must lie on a GPU")
     given = 0
     if tokens is not None:
         if tokens.dim() not in (1, 2) or tokens.shape[0] != M:
@@ -368,16 +387,18 @@ def logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None, top: int 
         d.given, d.tokens = given, _integers("tokens", tokens, _INT64, M * given)
     if out is None:
         out = logprobs_buffers(logits, given, top, entropy)
-    for name, t, shape, dtype in (("given", out.given, (M, given) if given else None, torch.float32), ("entropy", out.entropy, (M,), torch.float32),
-                                  ("top_ids", out.top_ids, (M, top) if top else None, _INT64), ("top", out.top, (M, top) if top else None, torch.float32)):
+    for name, t, wanted in (("given", out.given, given), ("entropy", out.entropy, 0), ("top_ids", out.top_ids, top), ("top", out.top, top)):
         if t is None:
-            if shape is not None and name != "entropy":
+            if wanted:
                 raise ValueError(f"out.{name} is missing")
-        elif t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
-            raise ValueError(f"out.{name} must be a contiguous {dtype} tensor {list(shape or ())}")
-    d.given_out, d.entropy, d.top_ids, d.top_out = (None if t is None else t.data_ptr() for t in out)
+        elif t.dtype is not (_INT64 if name == "top_ids" else torch.float32) or t.shape != ((M,) if name == "entropy" else (M, wanted)) or \
+                not t.is_contiguous() or (wanted == 0 and name != "entropy"):
+            raise ValueError(f"out.{name} must be a contiguous tensor {[M] if name == 'entropy' else [M, wanted]} of its type, and None where nothing is asked for")
     ws = getattr(out, "workspace", None)          # of a plain tuple there is none: no row is shared then
-    device = _device_of(logits, tokens, ws, *out)
+    for t in (tokens, ws, *out):
+        if t is not None and t.get_device() != device:
+            raise ValueError("the tensors of a call must lie on one GPU")
+    d.given_out, d.entropy, d.top_ids, d.top_out = (None if t is None else t.data_ptr() for t in out)
     at_ws, ws_bytes = (0, 0) if ws is None else (ws.data_ptr(), ws.numel())
     if device != _current_device():
         with torch.cuda.device(device):
