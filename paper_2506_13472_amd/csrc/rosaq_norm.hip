@@ -34,13 +34,17 @@ template <int TEAM, class T, class F> __device__ __forceinline__ T reduce(T v, T
   return v;
 }
 
+// A team of more than a wave is a workgroup, whose LDS and barriers it has alone.
+constexpr int threads_of(int team) { return team > 64 ? team : 256; }
+
 // ADD 0: no residual, 1: fp16, 2: fp32.  The sum of squares is fp32, of rows whose residual is fp32 in fp64: those may hold numbers whose squares
 // fp32 does not.  CODES: all in fp64, because a code next to a border is a whole step off when it falls to the other side; a step is a 127th of the largest
-// value.  The vector units bound it then, most of all the conversions to fp64 (1003 x 5120 with an fp32 residual 14.1 us, of which memory 11.5; 8192 x 4096 with
-// an fp16 one 69 and 48).  Built and slower: fp32, and fp64 again for what fp32 cannot decide (22.3 and 61 us: a branch a channel).
+// value.  The vector units bound it then: the conversions to fp64, and a row's own part (reductions, root, quotients), which every wave of it pays (1003 x 5120
+// with an fp32 residual 14.2 us, of which memory 11.5; 8192 x 4096 with an fp16 one 49 and 48, without one 31 and 20).  Built and slower: fp32, and fp64 again
+// for what fp32 cannot decide (22 and 61 us for the first two: a branch a channel).
 template <int TEAM, int CH, int ADD, bool CODES>
-__global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void rmsnorm_kernel(NormArgs a) {
-  constexpr int kThreads = TEAM < 256 ? 256 : TEAM, kTeams = kThreads / TEAM;
+__global__ __launch_bounds__(threads_of(TEAM)) void rmsnorm_kernel(NormArgs a) {
+  constexpr int kThreads = threads_of(TEAM), kTeams = kThreads / TEAM;
   constexpr bool F32 = ADD == 2, kHold = CODES && !(TEAM == 1024 && CH > 2);      // there the registers are too few
   using Sum = std::conditional_t<F32 || CODES, double, float>;
   using Value = std::conditional_t<CODES, double, float>;
@@ -90,6 +94,7 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void rmsnorm_kernel(NormAr
       if constexpr (kHold) return wide[i][j];
       else return h(i, j);
     };
+    // the sum rounded to fp32 is the same from fp32 operands as from fp64's; of an fp32 residual it is at hand in fp64 (8192 x 4096 to codes 71 us, 76 from fp32)
     if constexpr (ADD != 0) {
       if (a.residual_out) {
 #pragma unroll
@@ -106,7 +111,7 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void rmsnorm_kernel(NormAr
           } else {
             half8 o;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] = static_cast<_Float16>(static_cast<float>(held(i, j)));
+            for (int j = 0; j < 8; ++j) o[j] = static_cast<_Float16>(static_cast<float>(as_h8(x[i])[j]) + channel<F32>(r[i], j));
             reinterpret_cast<uint4*>(static_cast<_Float16*>(a.residual_out) + row * a.ld_residual_out)[p] = __builtin_bit_cast(uint4, o);
           }
         }
@@ -116,8 +121,8 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void rmsnorm_kernel(NormAr
     // of rows whose residual is fp32 the factor may be beyond fp32, and its power of two goes to h first
     Value factor;
     int power = 0;
-    if constexpr (CODES) factor = 1.0 / sqrt(sum / a.D + a.eps);
-    else if constexpr (F32) factor = static_cast<float>(frexp(1.0 / sqrt(sum / a.D + a.eps), &power));
+    if constexpr (CODES) factor = rsqrt(sum / a.D + a.eps);
+    else if constexpr (F32) factor = static_cast<float>(frexp(rsqrt(sum / a.D + a.eps), &power));
     else factor = 1.f / sqrtf(sum / static_cast<float>(a.D) + static_cast<float>(a.eps));
     auto formed = [&](int i, int j) {
       Value v = held(i, j);
@@ -185,34 +190,35 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void rmsnorm_kernel(NormAr
 }
 
 template <int TEAM, int CH, int ADD, bool CODES> static void run(const NormArgs& a, hipStream_t st) {
-  constexpr int kThreads = TEAM < 256 ? 256 : TEAM, kTeams = kThreads / TEAM;
+  constexpr int kThreads = threads_of(TEAM), kTeams = kThreads / TEAM;
   const int64_t groups = (static_cast<int64_t>(a.M) + kTeams - 1) / kTeams;
   rmsnorm_kernel<TEAM, CH, ADD, CODES><<<static_cast<unsigned>(std::min<int64_t>(groups, 1 << 20)), kThreads, 0, st>>>(a);
 }
 
+template <int TEAM, int CH, bool CODES> static void run(const NormArgs& a, hipStream_t st) {
+  if (!a.residual) run<TEAM, CH, 0, CODES>(a, st);
+  else if (!a.residual_f32) run<TEAM, CH, 1, CODES>(a, st);
+  else run<TEAM, CH, 2, CODES>(a, st);
+}
+
 template <int TEAM, int CH> static void run(const NormArgs& a, hipStream_t st) {
-  const int add = !a.residual ? 0 : (a.residual_f32 ? 2 : 1);
-  if (a.codes) {
-    if (add == 0) run<TEAM, CH, 0, true>(a, st);
-    else if (add == 1) run<TEAM, CH, 1, true>(a, st);
-    else run<TEAM, CH, 2, true>(a, st);
-  } else {
-    if (add == 0) run<TEAM, CH, 0, false>(a, st);
-    else if (add == 1) run<TEAM, CH, 1, false>(a, st);
-    else run<TEAM, CH, 2, false>(a, st);
-  }
+  if (a.codes) run<TEAM, CH, true>(a, st);
+  else run<TEAM, CH, false>(a, st);
 }
 
 // The smallest team whose threads hold one or two pieces each: more loads under way beside each other, fewer registers.  us with 256 threads / 512 / 1024: 8192 x
 // 4096 with an fp16 residual 45.0 / 41.5 / 47.6, 64 of them 3.4 / 2.9 / 3.1; 8192 x 5120 64.1 / 60.2 / 66.5, 64 of them 4.1 / 3.4 / 3.4; a wave
-// a row is slower still (8192 x 4096 52.4, 64 of them 6.7).
+// a row is slower still (8192 x 4096 52.4, 64 of them 6.7).  To codes of up to 4096 channels two pieces each, which halve the waves that a row's own part is paid
+// in: 8192 x 4096 without a residual 42.7 us in 512 threads, 32.0 in 256, 8192 x 2048 with an fp16 one 28.1 in 256, 26.6 in 128; 1003 x 5120 15.3 in 512, 15.8 in 256.
 int launch_rmsnorm(const NormArgs& a, void* stream) {
   hipStream_t st = static_cast<hipStream_t>(stream);
   const int pieces = a.D / 8;
   if (pieces <= 16) run<16, 1>(a, st);
   else if (pieces <= 64) run<64, 1>(a, st);
-  else if (pieces <= 256) run<256, 1>(a, st);
-  else if (pieces <= 512) run<512, 1>(a, st);
+  else if (pieces <= 256 && a.codes) run<128, 2, true>(a, st);
+  else if (pieces <= 256) run<256, 1, false>(a, st);
+  else if (pieces <= 512 && a.codes) run<256, 2, true>(a, st);
+  else if (pieces <= 512) run<512, 1, false>(a, st);
   else if (pieces <= 1024) run<512, 2>(a, st);
   else if (pieces <= 2048) run<1024, 2>(a, st);
   else run<1024, 4>(a, st);
