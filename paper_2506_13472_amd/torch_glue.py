@@ -353,6 +353,10 @@ _LOGITS = {torch.float16: B.F16, torch.bfloat16: B.BF16, torch.float32: B.F32}
 def logprobs_buffers(logits: torch.Tensor, given: int = 0, top: int = 0, entropy: bool = True) -> LogProbs:
     """Outputs for calls of logprobs over logits of this shape, for loops that keep them, with a workspace.  Calls with one must not overlap
     in time."""
+    if logits.dim() != 2 or logits.dtype not in _LOGITS:
+        raise ValueError("logits must be [M, V] in fp16, bf16 or fp32")
+    if given < 0 or top < 0:
+        raise ValueError(f"{given} given tokens and {top} alternatives: neither can be below zero")
     M, V = logits.shape
     device, real = logits.device, torch.float32
     out = LogProbs(torch.empty((M, given), dtype=real, device=device) if given else None,
@@ -370,10 +374,10 @@ def logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None, top: int 
     """rosaq_logprobs of logits [M, V] (fp16, bf16 or fp32): of tokens int64 [M, given], or [M] for one of each row (below zero: padding), and
     of the `top` largest, with the entropy.  out (logprobs_buffers) says instead of `entropy` whether that is wanted."""
     shape, device = logits.shape, logits.get_device()
-    M, V = shape
     kind = _LOGITS.get(logits.dtype)
-    if kind is None:
-        raise ValueError("logits must be fp16, bf16 or fp32")
+    if len(shape) != 2 or kind is None:
+        raise ValueError("logits must be [M, V] in fp16, bf16 or fp32")
+    M, V = shape
     d = B.LogprobsDesc()
     d.M, d.V, d.type, d.scale, d.top = M, V, kind, scale, top
     d.ld, d.logits = _beside("logits", logits, shape, logits.dtype, device), logits.data_ptr()

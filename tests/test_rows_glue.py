@@ -36,3 +36,15 @@ def test_buffers():
     out = T.logprobs_buffers(x, given=2, top=3)
     assert [tuple(t.shape) for t in out] == [(4, 2), (4,), (4, 3), (4, 3)] and out.top_ids.dtype is torch.int64 and out.workspace.numel() == 256
     assert T.logprobs_buffers(x, entropy=False) == (None, None, None, None)
+
+
+def test_buffers_refusals():
+    x = torch.zeros((4, 50), dtype=half)
+    for bad in (x.double(), x.long(), x[0], x[None]):
+        with pytest.raises(ValueError, match="in fp16, bf16 or fp32"):
+            T.logprobs_buffers(bad)
+        with pytest.raises(ValueError, match="in fp16, bf16 or fp32"):
+            T.logprobs(bad)
+    for kw in (dict(given=-1), dict(top=-2)):
+        with pytest.raises(ValueError, match="below zero"):
+            T.logprobs_buffers(x, **kw)
