@@ -123,16 +123,16 @@ def test_window_offsets_beyond_32_bits_and_strides():
     T.cache_append(cache, dev(slots), dev(k), dev(v))
     for m in (1, rows):
         q = rng.standard_normal((m, 1024)).astype(np.float16)
-        wide = torch.full((m, 3072), 7.0, dtype=torch.float16, device="cuda")
+        wide = torch.full((m, 3584), 7.0, dtype=torch.float16, device="cuda")
         wide[:, :1024] = dev(q)
         plan = T.AttentionPlan(cache, 8, 1, max_kv=768, max_rows=m, window=window, sinks=sinks)
-        T.attention(plan, wide[:, :1024], dev(np.array([n], np.int32)), dev(pages), row_start=dev(np.array([0, m], np.int32)), out=wide[:, 2048:])
+        T.attention(plan, wide[:, :1024], dev(np.array([n], np.int32)), dev(pages), row_start=dev(np.array([0, m], np.int32)), out=wide[:, 2560:])
         p, j = np.arange(n - m, n)[:, None], np.arange(n)[None]
         mask = (j <= p) & ((j > p - window) | (j < sinks))
         pick = [0, m // 2, m - 1] if m > 1 else [0]
         want, bound = A.attention(q.reshape(m, 8, 128)[pick], A.held(k, 8, 8), A.held(v, 8, 8), mask[pick], 128 ** -0.5)
-        got = wide[:, 2048:].cpu().numpy().reshape(m, 8, 128)[pick].astype(np.float64)
-        assert np.all(np.abs(got - want) <= bound) and bool((wide[:, 1024:2048] == 7.0).all())
+        got = wide[:, 2560:].cpu().numpy().reshape(m, 8, 128)[pick].astype(np.float64)
+        assert np.all(np.abs(got - want) <= bound) and bool((wide[:, 1024:2560] == 7.0).all())
 
 
 @pytest.mark.parametrize("rows", [1, 6, 90])
