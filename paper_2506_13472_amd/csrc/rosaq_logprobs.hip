@@ -9,18 +9,20 @@
 // THREADS-th piece of 16 bytes) and where that was.  Of 256 groups of threads the top-th largest (or some of those next to it) is a bound that at least
 // `top` logits reach, and only in the shares of threads whose largest does: about `top` shares of a THREADS-th of the row.  Those are read
 // again (from a cache, mostly), what reaches the bound goes to a list in LDS, and every member counts how many are before it.
-// A bound without a search, the least of `top` groups' largest, lets three times as many logits through, and cost more on the list than the search
-// (64 rows of 32000, five of each: 11.2 us against 8.5).
+// A bound that lets three times as many logits through (the least of `top` groups' largest) cost more on the list than it saved (64 rows of 32000, five
+// of each: 11.2 us against 8.5); a search for it, bit by bit, in place of the count that up to 32 alternatives take, 8.9 against 8.2.
 //
 // Order is by value and of equal values by the lower index, so that the answer does not depend on who finds what when.  The bound is of the same order: a
 // value, and the last piece in which that value counts.  A row of one value throughout (or of few logits and -inf besides) so has a short list too.
 // Where the list would be longer than its place, which takes a row whose largest logits nearly all lie in few threads' shares, the bound is
 // found by bisection over the whole row.
 //
-// Many rows are bound by memory (4095 x 32000 fp16 43 us in a loop of its own = 6.1 TB/s, with five alternatives 54, with twenty 69): a logit takes some eleven vector operations and an
-// exponential, two thirds of the time that it takes to come.  Few rows are bound by one compute unit each: a row of 32000 is read in 3.5 us, the
-// alternatives take 2.9 more (search, shares, list and ranks one after the other: 64 rows 8.9 us, without them 6.0).  The next pieces fetched ahead of the
-// present ones' arithmetic were no faster (one row of 262144 32 us, 34 with it): what a compute unit can have under way is, with eight waves.
+// Many rows are bound by memory (4095 x 32000 fp16 43 us in a loop of its own = 6.1 TB/s, with five alternatives 49, with twenty 60): a logit takes some nine vector
+// operations and an exponential (four more), over half of the time that it takes to come.  Few rows are bound by the same arithmetic in one compute unit each: 64
+// rows of 32000 take 5.3 us (6.0 with the conversion apart), and with five alternatives 8.0: bound, shares, list and ranks, one after the other, a few
+// hundred ns of latency each.  Built and no faster: the next pieces fetched ahead (one row of 262144 34 us against 32); d as one product and difference, with
+// a whole number in place of m a log2 e and the other way where that is too large for it (7.9 and 5.2, but 4096 rows of 1000 19.4 against 18.0); every wave
+// looking through its own threads' shares, without a list of those (8.2).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -89,6 +91,20 @@ template <class K> struct Row {
     if constexpr (K::kShift == 13) return static_cast<float>(as_h8(w)[j]);
     else if constexpr (K::kShift == 16) return __builtin_bit_cast(float, j % 2 ? (&w.x)[j / 2] & 0xffff0000u : (&w.x)[j / 2] << 16);
     else return __builtin_bit_cast(float, (&w.x)[j]);
+  }
+  // The largest element of a piece, NaN where one is NaN.
+  static __device__ __forceinline__ float most(const uint4& w) {
+    if constexpr (K::kShift == 13) {
+      typedef _Float16 half2 __attribute__((ext_vector_type(2)));
+      auto two = [](uint32_t v) { return __builtin_bit_cast(half2, v); };
+      const half2 a = __builtin_elementwise_maximum(__builtin_elementwise_maximum(two(w.x), two(w.y)), __builtin_elementwise_maximum(two(w.z), two(w.w)));
+      return larger(static_cast<float>(a[0]), static_cast<float>(a[1]));
+    } else {
+      float top = element(w, 0);
+#pragma unroll
+      for (int j = 1; j < K::kEach; ++j) top = larger(top, element(w, j));
+      return top;
+    }
   }
   // Of any piece: -inf in place of what is not the row's; the places (bits) of those that are.
   __device__ __forceinline__ uint32_t load_any(int piece, uint4* w) const {
@@ -206,8 +222,11 @@ __global__ __launch_bounds__(THREADS) void logprobs_kernel(LogprobArgs a) {
     uint32_t best_key = 0;                   // of this thread's share: the largest, 0 without one, and the first piece that holds it
     int best_piece = lo + tid;
     Bound best = 0;                          // the two as one
+    // v - m of an fp16 v as a product with a one that the compiler does not know: an instruction with the conversion in it
+    float one = 1.f;
+    asm("" : "+s"(one));
     auto add = [&](float v) {
-      const float d = fmaxf((v - sums.m) * c, kLeast), e = __builtin_amdgcn_exp2f(d);
+      const float d = fmaxf((K::kShift == 13 ? __builtin_fmaf(v, one, -sums.m) : v - sums.m) * c, kLeast), e = __builtin_amdgcn_exp2f(d);
       sums.s += e;
       sums.t = __builtin_fmaf(e, d, sums.t);
     };
@@ -223,9 +242,7 @@ __global__ __launch_bounds__(THREADS) void logprobs_kernel(LogprobArgs a) {
       float most = sums.m;
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
-        float top = x.element(w[u], 0);
-#pragma unroll
-        for (int j = 1; j < E; ++j) top = larger(top, x.element(w[u], j));
+        const float top = x.most(w[u]);
         if constexpr (TOP) {
           const uint32_t k = key_of(top);
           if (k > best_key && p0 + u * THREADS < end) { best_key = k; best_piece = p0 + u * THREADS; }
@@ -244,9 +261,7 @@ __global__ __launch_bounds__(THREADS) void logprobs_kernel(LogprobArgs a) {
       if (x.whole(p) || tid != (p - lo) % THREADS) continue;
       uint4 w;
       x.load_any(p, &w);
-      float top = x.element(w, 0);
-#pragma unroll
-      for (int j = 1; j < E; ++j) top = larger(top, x.element(w, j));
+      const float top = x.most(w);
       if constexpr (TOP) {
         const uint32_t k = key_of(top);
         if (k > best_key || (k == best_key && p < best_piece)) { best_key = k; best_piece = p; }
@@ -286,20 +301,24 @@ __global__ __launch_bounds__(THREADS) void logprobs_kernel(LogprobArgs a) {
         uint32_t lane_most = k[0];
 #pragma unroll
         for (int i = 1; i < kGroups / 64; ++i) lane_most = max(lane_most, k[i]);
-        const uint32_t most = wave_all(lane_most, [](uint32_t a, uint32_t b) { return max(a, b); });
-        // groups that reach a key; for few alternatives four of them are counted as one, which lets hardly more through and takes half as long
-        const bool few = a.top <= 32;
+        // groups that reach a key
         auto at_least = [&](uint32_t v) {
-          if (v > most) return 0;
-          int n = __popcll(__ballot(lane_most >= v));
-          if (few) return n;
-          n = 0;
+          int n = 0;
 #pragma unroll
           for (int i = 0; i < kGroups / 64; ++i) n += __popcll(__ballot(k[i] >= v));
           return n;
         };
-        // a row of few pieces has fewer groups than alternatives: all of it is on the list.  A few groups too many cost less than to tell them apart
-        const uint32_t key = reached_by<kBits>(a.top, 16, at_least);
+        // For few alternatives a lane's four groups are one, which lets hardly more through, and each lane counts the lanes above it; else a search.  A row of few
+        // pieces has fewer groups than alternatives: all of it is on the list.  In the search a few groups too many cost less than to tell them apart
+        uint32_t key;
+        if (a.top <= 32) {
+          int above = 0;
+#pragma unroll
+          for (int o = 0; o < 64; ++o) above += lane_of(lane_most, o) > lane_most ? 1 : 0;
+          key = wave_all(above < a.top ? lane_most : 0xffffffffu, [](uint32_t a, uint32_t b) { return min(a, b); });
+        } else {
+          key = reached_by<kBits>(a.top, 16, at_least);
+        }
         uint32_t last = 0;
         if (key != 0 && at_least(key) > a.top + 24)
           last = reached_by<32>(a.top, 16, [&](uint32_t v) {
@@ -444,7 +463,7 @@ static bool wide(const LogprobArgs& a) {
   return bytes > (a.M > 640 ? 65536 : 32768);
 }
 
-// A compute unit reads some 35 GB/s alone, so that few long rows are better shared by several, at the price of another launch.  us in 1 / 2 / 4 / 8 / 16
+// A compute unit alone takes some ten logits a ns, so that few long rows are better shared by several, at the price of another launch.  us in 1 / 2 / 4 / 8 / 16
 // parts, fp16, five alternatives: one row of 65536 10.7 / 10.5 / 9.2 / 9.6 / 10.1, of 262144 29.1 / 19.4 / 13.3 / 10.9 / 10.2; 64 of 131072 19.1 / 15.7 / 12.9 / 13.1 / 17.7;
 // 128 of 65536 12.7 / 12.8 / 13.0 / 17.3 / 25.4, of 262144 34.0 / 23.9 / 21.5 / 23.1 / 27.1; 257 of 32000 11.7 / 14.0 / 18.7 / 26.5 / 36.5.
 int parts_of_logprobs(const LogprobArgs& a) {
