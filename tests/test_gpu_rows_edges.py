@@ -12,7 +12,7 @@ from paper_2506_13472_amd import binding as B
 from paper_2506_13472_amd import torch_glue as T
 from test_gpu_attention import dev
 from test_gpu_attention_window import Windowed
-from test_gpu_logprobs import check, rows
+from test_gpu_logprobs import TYPES, check, rows
 from test_gpu_rmsnorm import close, coded, kept
 
 pytestmark = pytest.mark.gpu
@@ -31,6 +31,17 @@ def test_norm_of_more_rows_than_a_grid_has(M, D):
     close(y[some], R.rmsnorm(xs, None, 1e-5, rs)[1])
     kept(total[some], xs, rs)
     assert bool((y.abs().amax(dim=1) > 0).all())
+
+
+@pytest.mark.parametrize("M,D", [((1 << 20) + 5, 1032), ((1 << 20) + 300, 4096), ((1 << 22) + 9, 136)])
+def test_codes_of_more_rows_than_a_grid_has(M, D):
+    print(f"case rmsnorm codes {M} x {D}", flush=True)
+    x = torch.randn((4096, D), device="cuda").half().repeat(M // 4096 + 1, 1)[:M]
+    x[(1 << 20) - 1] = 0                       # its place's next row is not of zeros
+    codes, scales = T.rmsnorm_codes(x)
+    some = torch.cat((torch.arange(64), torch.arange((1 << 20) - 2, (1 << 20) + 5), torch.arange(M - 300, M), torch.randint(0, M, (200,)))).cuda()
+    coded(codes[some], scales[some], R.rmsnorm(x[some].cpu().numpy())[1])
+    assert int((codes.view(torch.int32) != 0).any(dim=1).sum()) == M - 1
 
 
 def test_norm_of_rows_past_32_bits():
@@ -84,6 +95,31 @@ def test_logprobs_read_nothing_beside_their_rows():
             for shift in range(9):
                 x = rows(2, V, kind, shift, pad=3, shift=shift)          # 300 in the gaps
                 check(x, torch.zeros((2, 1), dtype=torch.int64, device="cuda"), min(V, 9))
+
+
+@pytest.mark.parametrize("kind", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("top", [2, 31, 32, 33])
+def test_alternatives_from_a_count_and_from_a_search(top, kind):
+    """Both ways to the bound: few and many values, all large ones in few threads' shares, rows of few pieces."""
+    for V in (40, 300, 9000, 40003, 140001):
+        print(f"case logprobs {top} of {V} {kind}", flush=True)
+        base = torch.arange(V, device="cuda")
+        x = torch.zeros((7, V), dtype=torch.float32, device="cuda")
+        x[1] = (base * 7919 % 3).float()
+        x[2] = (base * 40503 % 65536) / 65536.0
+        x[3] = torch.where(base % 4096 < 8, 6.0 + (base * 40503 % 65536) / 65536.0, -2.0 - base % 5)
+        x[4] = torch.where(base % 2048 < 4, 6.0 + (base * 40503 % 65536) / 65536.0, -2.0 - base % 5)
+        x[5] = torch.where(base < top - 1, 1.0, -np.inf)
+        x[6, V // 2] = np.nan
+        check(x.to(TYPES[kind]), base[:7].clone(), top)
+
+
+def test_small_scales_leave_nothing_of_minus_infinity():
+    for kind in ("f16", "bf16", "f32"):
+        print(f"case logprobs small scales {kind}", flush=True)
+        x = rows(3, 5000, kind, masked=0.5)
+        for a in (1e-3, 2.0 ** -20, 2.0 ** -60):
+            check(x, torch.tensor([1, 2, 3], device="cuda"), 5, a)
 
 
 def test_two_graphs_of_logprobs_share_a_workspace():
