@@ -55,12 +55,12 @@ __device__ __forceinline__ int steps_of(const AttendArgs& a, int over, int step,
 // that the first row's window begins in to the last row, and then over the sinks, where a gap lies behind them.  Tokens that no row of the tile
 // sees are neither counted on to be in the cache nor their pages to be the sequence's: of those that lie in the same step nothing is used.
 // Measured: 64 x 32 heads, window 1024, 4 bits 64.6 us (287 MB, 4.4 TB/s); one row's 32 heads, window 8191, 8 bits 20.5; four prompts of 2048 rows x 32 heads,
-// window 512, 8 bits 126 us = 480 TFLOP/s of what the mask leaves, where the whole triangle runs at 750: a tile has 11 stages then, not 17 on average, and
-// of its 38 us 5 go until the first codes are in LDS, 1.3 to the end, and the stages that some row does not see all of take 3.3 where others take 2.5.
+// window 512, 8 bits 120 us = 500 TFLOP/s of what the mask leaves, where the whole triangle runs at 750: a tile has 11 stages then, not 17 on average, and
+// of its 30 us some 5 go until the first codes are in LDS, 1.3 to the end, and the stages that some row does not see all of cost a third more than others.
 // Built and slower: steps over records of 16 tokens wherever they lie, which spares up to one in eleven stages but looks up four pages a stage (prompts 139 us
 // against 131, one row 21.9 against 20.7; odd windows 103 against 113), the sinks in free records of the first stage (136), their own records alone multiplied
-// within the loop (spills, 188), one comparison a score for each side's mask (as fast), one row tile a wave (144), the second and third stage's codes touched
-// ahead (139 against 136).  The sinks first cost a stage and the wait for its codes (131 against 127).
+// within the loop (spills, 188), one comparison a score for each side's mask (as fast as two), one row tile a wave (144), the second and third stage's codes touched
+// ahead (139 against 136); a wave's priority raised for its products (137 against 123, 4 bits).  The sinks first cost a stage and the wait for its codes (131 against 127).
 __device__ __forceinline__ int lowest(const AttendArgs& a, int tokens, int count, int i) { return max(tokens - count + i + 1 - a.window, 0); }
 struct Walk {
   int start = 0;           // token that the steps begin with
@@ -533,6 +533,12 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// The bits of 64 from this one on.
+__device__ __forceinline__ uint64_t from_bit(int n) {
+  const int m = min(max(n, 0), 64);
+  return ~uint64_t{0} << m / 2 << (m - m / 2);
+}
+
 template <int D, int BITS, int RT, bool W = false>
 __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLaunch& n, int parts, int block, StageLds<D> (&lds)[stage_buffers(RT)]) {
   constexpr int U = D / 16, KS = D / 32, kTileRows = 16 * RT * kWaves;
@@ -564,18 +570,20 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
   const int most_low = W ? lowest(a, tokens, rows.count, min(first_row + 16 * RT - 1, used - 1) / a.group) : 0;
   half8 q[RT][KS];
   int limit[RT];
+  auto load_queries = [&]() {
 #pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    const int my = min(first_row + 16 * t + r, used - 1), my_token = my / a.group;
-    limit[t] = visible(a, tokens, rows.count, my_token);
-    const _Float16* src = static_cast<const _Float16*>(a.q) + static_cast<int64_t>(rows.start + my_token) * a.ldq +
-                          (w.kv_head * a.group + my % a.group) * D + g * (D / 4);
+    for (int t = 0; t < RT; ++t) {
+      const int my = min(first_row + 16 * t + r, used - 1), my_token = my / a.group;
+      limit[t] = visible(a, tokens, rows.count, my_token);
+      const _Float16* src = static_cast<const _Float16*>(a.q) + static_cast<int64_t>(rows.start + my_token) * a.ldq +
+                            (w.kv_head * a.group + my % a.group) * D + g * (D / 4);
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      const half8 h = load_query(src + 8 * s);
-      q[t][s] = BITS == 4 ? half8{h[0], h[4], h[1], h[5], h[2], h[6], h[3], h[7]} : h;
+      for (int s = 0; s < KS; ++s) {
+        const half8 h = load_query(src + 8 * s);
+        q[t][s] = BITS == 4 ? half8{h[0], h[4], h[1], h[5], h[2], h[6], h[3], h[7]} : h;
+      }
     }
-  }
+  };
 
   const CacheDev& c = a.cache;
   const int block_shift = c.page_shift - 4;
@@ -658,7 +666,8 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int at = record * kCacheBlock + 4 * g + i;
-          if (at >= held || (x.hidden >> record & 1) || (W && t0 + at < walk.low && t0 + at >= a.sinks)) sz[b][i] = 0u;
+          const bool away = (at >= held) | ((x.hidden >> record & 1) != 0) | (W && ((t0 + at < walk.low) & (t0 + at >= a.sinks)));
+          sz[b][i] = away ? 0u : sz[b][i];
         }
       }
     }
@@ -731,17 +740,35 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
 #pragma unroll
         for (int i = 0; i < 4; ++i) score[b][t][i] = __builtin_fmaf(score[b][t][i], scale[i], -base[t]);
     }
-    if (masked) {
+    if (W && masked) {
+      // a bit for each token of the stage that a row does not see.  With two borders and the sinks faster than comparisons for each score (119.3 us against
+      // 123, 4 x 2048 rows x 32 heads, window 512, 4 bits), with one border slower
+      const uint64_t no_sinks = from_bit(a.sinks - t0);
+      uint64_t absent = 0;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) absent |= (hidden >> b & 1) ? uint64_t{0xffff} << 16 * b : 0;
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        const int lim = limit[t] - t0;         // a row's window begins `window` tokens before its limit
+        const uint64_t away = (from_bit(lim) | (no_sinks & ~from_bit(lim - a.window)) | absent) >> 4 * g;
+        const uint32_t half[2] = {static_cast<uint32_t>(away), static_cast<uint32_t>(away >> 32)};
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const bool off = half[b / 2] >> (16 * (b % 2) + i) & 1;
+            score[b][t][i] = off ? -INFINITY : score[b][t][i];
+          }
+      }
+    } else if (masked) {
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
           const int lim = (own ? limit[t] : a.prefix_len) - t0 - b * kCacheBlock - 4 * g;
-          // a row's window begins `window` tokens before its limit
-          const int low = W ? lim - a.window : 0, sinks = W ? a.sinks - t0 - b * kCacheBlock - 4 * g : 0;
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            score[b][t][i] = i < lim && !(hidden >> b & 1) && (!W || i >= low || i < sinks) ? score[b][t][i] : -INFINITY;
+            score[b][t][i] = i < lim && !(hidden >> b & 1) ? score[b][t][i] : -INFINITY;
         }
     }
     float most[RT];
@@ -801,6 +828,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
     Pages<4> next = pages_of(begin);
     load(begin, next, x);
     next = pages_of(begin + 1);
+    load_queries();           // behind the codes, which are waited for first
     store(begin, x, lds[0]);
     hidden = x.hidden;
     lds_barrier();
