@@ -32,6 +32,9 @@ static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // With a window sequences take about the same number of steps, and one round of workgroups, as many as are resident at a time (512 or 768), is better than
 // many: in 2048 / 768 / 512 workgroups 16 x (8 x 4) rows, window 4096, 4 bits 30.1 / 24.1 / 24.9 us, 128 x (8 x 4) heads of 64, window 1024 32.1 / 25.0 / 24.6;
 // 8 bits, one row of 32 heads, window 8191 23.0 / 22.9 / 21.3, 32 x (8 x 4), window 2048 37.7 / 37.7 / 35.8.
+// A few steps are better left whole, as two or three parts save less than the launch that joins them: us in parts / whole, 16 x (8 x 4) rows, window 450
+// 11.2 / 8.5, 900 14.0 / 13.0 (8 bits 15.3 / 13.3), 1024 13.9 / 14.3 (15.6 / 14.6), 1500 16.0 / 18.4; 32 x (8 x 4), 1024 17.6 / 15.0 (20.9 / 17.1); with fewer
+// workgroups parts are worth more: 4 x (8 x 4), window 512 9.6 / 8.9, 640 10.1 / 9.7, 768 9.7 / 10.6.
 // Waves alone: where there are 2048 tiles of up to 16 steps (64 x 32 heads, us together / alone: 256 tokens 20.6 / 19.3, 512 34.2 / 32.3, 1024
 // 52.5 / 54.8).
 static AttendLaunch shape_launch(const AttendArgs& a, int over, int64_t rows, int64_t tokens_prefix, int64_t tokens_own, int64_t seqs) {
@@ -40,17 +43,20 @@ static AttendLaunch shape_launch(const AttendArgs& a, int over, int64_t rows, in
   n.row_tiles = rows <= kRows && over != kPrefix ? 0 : (rows <= 64 ? 1 : 2);
   n.tiles = static_cast<int>(ceil_div(rows, n.row_tiles ? 16 * n.row_tiles * kWaves : kRows));
   const int step = n.row_tiles ? kStage : kStep;
-  int64_t all = std::max<int64_t>(1, ceil_div(tokens_prefix, step) + ceil_div(tokens_own, step));
+  const int64_t everything = std::max<int64_t>(1, ceil_div(tokens_prefix, step) + ceil_div(tokens_own, step));
+  int64_t all = everything;
   if (a.window) {
     // the sinks, and from the step that the first row's window begins in to the last of a tile's rows
     const int64_t tile_rows = n.row_tiles ? 16 * n.row_tiles * kWaves : kRows;
     const int64_t apart = std::min<int64_t>(ceil_div(tile_rows - 1, a.group), a.max_rows - 1);
     all = std::min<int64_t>(all, ceil_div(a.sinks, step) + ceil_div(static_cast<int64_t>(a.window) + apart + step - 1, step));
   }
+  const bool narrow = all < everything;      // a window over everything takes the parts, and so adds in the order, of a call without one
   const int64_t pairs = seqs * a.cache.kv_heads, groups = pairs * n.tiles;
   const int64_t resident = 256 * (a.dim == 128 && a.bits == 8 ? 2 : 3);      // workgroups of attend_rows, by its registers
-  const int64_t fill = n.row_tiles == 0 ? (a.window ? resident : 2048) : (n.row_tiles == 1 && over == kPrefix ? 256 : 512);
-  const int64_t parts = std::clamp<int64_t>(fill / groups, 1, std::max<int64_t>(1, all / (n.row_tiles ? 2 : 8)));
+  const int64_t fill = n.row_tiles == 0 ? (narrow ? resident : 2048) : (n.row_tiles == 1 && over == kPrefix ? 256 : 512);
+  const bool whole = narrow && (all < 20 || (all < 36 && groups >= 96));
+  const int64_t parts = std::clamp<int64_t>(fill / groups, 1, std::max<int64_t>(1, n.row_tiles ? all / 2 : (whole ? 1 : all / 8)));
   n.steps = static_cast<int>(ceil_div(all, parts));
   n.parts = static_cast<int>(ceil_div(all, n.steps));
   n.alone = n.row_tiles == 0 && groups * n.parts >= 2048 && n.steps <= 16;

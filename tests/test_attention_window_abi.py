@@ -79,6 +79,22 @@ def test_parts_hold_all_steps(group, max_rows, window, sinks):
     assert _parts(window, sinks, 1, group, max_rows, 1, max_rows, max_kv) == -(-bound // steps)
 
 
+@pytest.mark.parametrize("seqs,kv,rows", [(1, 1, 1), (3, 2, 1), (16, 8, 1), (64, 8, 2), (5, 2, 12), (2, 4, 100)])
+def test_parts_of_a_window_over_everything_are_those_without_one(seqs, kv, rows):
+    for max_kv in (1, 64, 300, 512, 640, 1024, 1100, 5000):
+        want = _parts(0, 0, kv, 1, seqs * rows, seqs, rows, max_kv)
+        for window, sinks in ((max_kv, 0), (1 << 30, 0), (1, max_kv), (max_kv, max_kv)):
+            assert _parts(window, sinks, kv, 1, seqs * rows, seqs, rows, max_kv) == want
+
+
+def test_few_steps_stay_whole():
+    # a window of w that begins anywhere in a step of 32 tokens takes up to (w + 31) / 32, rounded up, of them, and four sinks one: 560 take 19 + 1, 1024 33 + 1
+    for window, whole in ((100, True), (500, True), (560, False), (640, False)):
+        assert (_parts(window, 4, 8, 4, 4, 4, 1, 4000) == 1) == whole
+    for window, whole in ((640, True), (1024, True), (1100, False)):
+        assert (_parts(window, 4, 8, 4, 16, 16, 1, 4000) == 1) == whole
+
+
 def test_torch_plan_refusals():
     torch = pytest.importorskip("torch")
     from paper_2506_13472_amd import torch_glue as T
