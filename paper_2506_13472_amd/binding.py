@@ -185,6 +185,13 @@ def _check(rc: int):
         raise RosaqError(rc, rosaq_last_error())
 
 
+def int32(*numbers: int):
+    """Refuses numbers that an int32 of the C ABI does not hold: ctypes would pass on their low 32 bits."""
+    for n in numbers:
+        if not -0x80000000 <= n <= 0x7fffffff:
+            raise RosaqError(-2, f"{n} is beyond int32")
+
+
 def _ptr(a):
     return None if a is None else a.ctypes.data_as(C.c_void_p)
 
@@ -329,6 +336,7 @@ def rosaq_pca_full(x_ptr: int, n_cal: int, D: int, ldx: int, stream: int = 0):
 
 
 def rosaq_cache_bytes(kv_heads: int, head_dim: int, bits: int, page_tokens: int, num_pages: int) -> int:
+    int32(kv_heads, head_dim, bits, page_tokens, num_pages)
     n = lib().rosaq_cache_bytes(kv_heads, head_dim, bits, page_tokens, num_pages)
     if n == 0:
         raise RosaqError(-2, rosaq_last_error())
@@ -369,6 +377,7 @@ def rosaq_attention(desc: AttentionDesc, ws_ptr: int, ws_bytes: int, stream: int
 
 
 def rosaq_workspace_bytes_attention_window(desc: AttentionDesc, window: int, sinks: int) -> int:
+    int32(window, sinks)
     n = lib().rosaq_workspace_bytes_attention_window(C.byref(desc), window, sinks)
     if n == 0:
         raise RosaqError(-2, rosaq_last_error())
@@ -376,6 +385,8 @@ def rosaq_workspace_bytes_attention_window(desc: AttentionDesc, window: int, sin
 
 
 def rosaq_attention_window(desc: AttentionDesc, window: int, sinks: int, ws_ptr: int, ws_bytes: int, stream: int = 0):
+    if (window | sinks) >> 31:          # a call of a few us: the loop only where a number may be refused
+        int32(window, sinks)
     _check(lib().rosaq_attention_window(desc, window, sinks, ws_ptr, ws_bytes, stream))
 
 

@@ -208,6 +208,7 @@ class AttentionPlan:
         self.M, self.width, self.sequences, self.prefix_len = sequences * max_rows if rows is None else rows, q_heads * cache.head_dim, sequences, prefix_len
         self.desc = B.AttentionDesc()
         d = self.desc
+        B.int32(q_heads, self.M, sequences, max_kv, max_rows, prefix_len)
         d.cache = C.pointer(cache.args)
         d.q_heads, d.M, d.sequences, d.max_kv, d.max_rows, d.prefix_len = q_heads, self.M, sequences, max_kv, max_rows, prefix_len
         d.causal, d.scale = int(causal), cache.head_dim ** -0.5 if scale is None else scale
@@ -276,6 +277,8 @@ def _rmsnorm(x, weight, eps, residual, residual_out, y, codes, scales):
     """One rosaq_rmsnorm call on x's device; y, codes and scales: None, or where they go."""
     shape, device = x.shape, x.get_device()
     M, D = shape
+    if (M | D) >> 31:
+        B.int32(M, D)
     d = B.RmsNormDesc()
     d.M, d.D, d.eps = M, D, eps
     d.ldx, d.x = _beside("x", x, shape, _HALF, device), x.data_ptr()
@@ -358,6 +361,7 @@ def logprobs_buffers(logits: torch.Tensor, given: int = 0, top: int = 0, entropy
     if given < 0 or top < 0:
         raise ValueError(f"{given} given tokens and {top} alternatives: neither can be below zero")
     M, V = logits.shape
+    B.int32(M, V, given, top)
     device, real = logits.device, torch.float32
     out = LogProbs(torch.empty((M, given), dtype=real, device=device) if given else None,
                    torch.empty(M, dtype=real, device=device) if entropy else None,
@@ -378,17 +382,20 @@ def logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None, top: int 
     if len(shape) != 2 or kind is None:
         raise ValueError("logits must be [M, V] in fp16, bf16 or fp32")
     M, V = shape
-    d = B.LogprobsDesc()
-    d.M, d.V, d.type, d.scale, d.top = M, V, kind, scale, top
-    d.ld, d.logits = _beside("logits", logits, shape, logits.dtype, device), logits.data_ptr()
-    if device < 0:
-        raise ValueError("the tensors of a call must lie on a GPU")
     given = 0
     if tokens is not None:
         if tokens.dim() not in (1, 2) or tokens.shape[0] != M:
             raise ValueError(f"tokens must be [{M}, given] or [{M}]")
         given = 1 if tokens.dim() == 1 else tokens.shape[1]
-        d.given, d.tokens = given, _integers("tokens", tokens, _INT64, M * given)
+    if (M | V | given | top) >> 31:
+        B.int32(M, V, given, top)
+    d = B.LogprobsDesc()
+    d.M, d.V, d.type, d.scale, d.given, d.top = M, V, kind, scale, given, top
+    d.ld, d.logits = _beside("logits", logits, shape, logits.dtype, device), logits.data_ptr()
+    if tokens is not None:
+        d.tokens = _integers("tokens", tokens, _INT64, M * given)
+    if device < 0:
+        raise ValueError("the tensors of a call must lie on a GPU")
     if out is None:
         out = logprobs_buffers(logits, given, top, entropy)
     for name, t, wanted in (("given", out.given, given), ("entropy", out.entropy, 0), ("top_ids", out.top_ids, top), ("top", out.top, top)):
