@@ -2,6 +2,7 @@
 #include "rosaq_rows.h"
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <string>
 
@@ -78,6 +79,9 @@ static int check_rmsnorm(const rosaq_rmsnorm_desc* d, NormArgs* a) {
   a->residual = d->residual_dev; a->ld_residual = d->ld_residual;
   a->residual_out = d->residual_out_dev; a->ld_residual_out = d->ld_residual_out;
   a->residual_f32 = d->residual_dev && d->residual_type == ROSAQ_F32;
+  // Where the kernel adds eps in fp32 it is kept to that type's normal numbers.  2^-126 is nothing beside the least mean square of fp16 numbers, 2^-48 / D, and
+  // keeps a row of zeros from 0 / 0 as a smaller eps does; with the largest one, as with any beyond it, every y is zero but an infinite weight's
+  if (!a->residual_f32 && !d->codes_dev && d->eps > 0.0) a->eps = std::clamp<double>(d->eps, FLT_MIN, FLT_MAX);
   a->weight = d->weight_dev;
   a->y = d->y_dev; a->ldy = d->ldy;
   a->codes = d->codes_dev; a->ld_codes = d->ld_codes; a->scales = d->scales_dev;
