@@ -174,7 +174,8 @@ template <int N> __device__ __forceinline__ Sums sums_of(const float (&m)[N], co
 struct Answer {
   float m, scale, log2_s, share;       // share: T / S
   __device__ Answer(const Sums& a, float scale) : m(a.m), scale(scale), log2_s(log2f(a.s)), share(a.t / a.s) {}
-  __device__ __forceinline__ float log_p(float x) const { return (x - m) * scale - log2_s * 0.6931471805599453f; }
+  // The difference by halves, exact but for subnormal numbers: that of logits at both ends of fp32's range is beyond it, its product with the scale need not be.
+  __device__ __forceinline__ float log_p(float x) const { return (0.5f * x - 0.5f * m) * (2.f * scale) - log2_s * 0.6931471805599453f; }
   __device__ __forceinline__ float entropy() const { return (log2_s - share) * 0.6931471805599453f; }
 };
 // The given tokens of a row, in two steps, so that nothing waits for them: `step` threads take them in turn, and the first round's are fetched ahead.
