@@ -282,8 +282,6 @@ def _rmsnorm(x, weight, eps, residual, residual_out, y, codes, scales):
     d = B.RmsNormDesc()
     d.M, d.D, d.eps = M, D, eps
     d.ldx, d.x = _beside("x", x, shape, _HALF, device), x.data_ptr()
-    if device < 0:
-        raise ValueError("the tensors of a call must lie on a GPU")
     if weight is not None:
         if weight.dtype is not _HALF or weight.shape != shape[1:] or not weight.is_contiguous() or weight.get_device() != device:
             raise ValueError(f"weight must be a contiguous fp16 tensor [{D}] on x's GPU")
@@ -308,6 +306,8 @@ def _rmsnorm(x, weight, eps, residual, residual_out, y, codes, scales):
         if scales.dtype is not torch.float32 or scales.shape != shape[:1] or not scales.is_contiguous() or scales.get_device() != device:
             raise ValueError(f"scales must be a contiguous fp32 tensor [{M}] on x's GPU")
         d.scales = scales.data_ptr()
+    if device < 0:
+        raise ValueError("the tensors of a call must lie on a GPU")
     if device != _current_device():
         with torch.cuda.device(device):
             B.rosaq_rmsnorm(d, _stream_on(device))
@@ -394,8 +394,6 @@ def logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None, top: int 
     d.ld, d.logits = _beside("logits", logits, shape, logits.dtype, device), logits.data_ptr()
     if tokens is not None:
         d.tokens = _integers("tokens", tokens, _INT64, M * given)
-    if device < 0:
-        raise ValueError("the tensors of a call must lie on a GPU")
     if out is None:
         out = logprobs_buffers(logits, given, top, entropy)
     for name, t, wanted in (("given", out.given, given), ("entropy", out.entropy, 0), ("top_ids", out.top_ids, top), ("top", out.top, top)):
@@ -409,6 +407,8 @@ def logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None, top: int 
     for t in (tokens, ws, *out):
         if t is not None and t.get_device() != device:
             raise ValueError("the tensors of a call must lie on one GPU")
+    if device < 0:
+        raise ValueError("the tensors of a call must lie on a GPU")
     d.given_out, d.entropy, d.top_ids, d.top_out = (None if t is None else t.data_ptr() for t in out)
     at_ws, ws_bytes = (0, 0) if ws is None else (ws.data_ptr(), ws.numel())
     if device != _current_device():
