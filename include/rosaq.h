@@ -411,7 +411,7 @@ int rosaq_attention_window(const rosaq_attention_desc* desc, int32_t window, int
  * residual in fp64), and rounded to fp16 once.  So a sum that fp16 does not hold is infinite in residual_out and right in y.
  * Optionally (or instead of y) as codes of 8 bits, for a product that takes those:
  *     scale = fp32(max |y| / 127),  code = rne(y / scale) in [-127, 127],  value code * scale
- * from a y in fp64.  A row of zeros has scale 0; one with NaN, or an infinity, in y has scale NaN and codes 0.
+ * from a y in fp64, h's sum too.  A row of zeros has scale 0; one with NaN, or an infinity, in y has scale NaN and codes 0.
  * A row that holds an infinity is zero but there, where it is NaN; one of zeros with eps 0 is NaN. */
 typedef struct {
   int32_t M, D;                      /* rows; channels: a multiple of 8 in [8, 32768]                    */

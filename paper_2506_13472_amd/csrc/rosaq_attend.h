@@ -54,9 +54,10 @@ __device__ __forceinline__ int steps_of(const AttendArgs& a, int over, int step,
 // With a window (W) row i, at position p = tokens - count + i, sees token j <= p if j > p - window or j < sinks.  A tile's steps then go from the whole step
 // that the first row's window begins in to the last row, and then over the sinks, where a gap lies behind them.  Tokens that no row of the tile
 // sees are neither counted on to be in the cache nor their pages to be the sequence's: of those that lie in the same step nothing is used.
-// Measured: 64 x 32 heads, window 1024, 4 bits 64.6 us (287 MB, 4.4 TB/s); one row's 32 heads, window 8191, 8 bits 20.5; four prompts of 2048 rows x 32 heads,
-// window 512, 8 bits 120 us = 500 TFLOP/s of what the mask leaves, where the whole triangle runs at 750: a tile has 11 stages then, not 17 on average, and
-// of its 30 us some 5 go until the first codes are in LDS, 1.3 to the end, and the stages that some row does not see all of cost a third more than others.
+// Measured: 64 x 32 heads, window 1024, 4 bits 63 us (287 MB, 4.6 TB/s), heads of 64 channels 49: half of the bytes, but three quarters of the vector operations,
+// which are 60 % of its cycles; one row's 32 heads, window 8191, 8 bits 20.5; four prompts of 2048 rows x 32 heads, window 512, 8 bits 121 us = 500 TFLOP/s of
+// what the mask leaves, where the whole triangle runs at 750: a tile has 11 stages then, not 17 on average, and of its 30 us some 5 go until the first codes are
+// in LDS, 1.3 to the end, and the stages that some row does not see all of cost a third more than others.
 // Built and slower: steps over records of 16 tokens wherever they lie, which spares up to one in eleven stages but looks up four pages a stage (prompts 139 us
 // against 131, one row 21.9 against 20.7; odd windows 103 against 113), the sinks in free records of the first stage (136), their own records alone multiplied
 // within the loop (spills, 188), one comparison a score for each side's mask (as fast as two), one row tile a wave (144), the second and third stage's codes touched
@@ -503,7 +504,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const AttendLau
 // Built and slower: eight waves a workgroup with half of them half a stage behind (233 against 189 us: the barriers
 // cost more than the sharing saves), the factors of the next stage between the MFMAs by the scheduler's groups (spills; 260
 // against 239 on the 4-bit chunk), three and four row tiles a wave (spills), half a stage at a time and one stage's LDS for three workgroups
-// a unit (spills), priorities around either product (none or worse), the first codes before the queries (188 against 186).
+// a unit (spills), priorities around either product (none or worse).
 constexpr int kStage = 4 * kCacheBlock;
 
 template <int D, int BITS> struct StageCodes {
@@ -828,7 +829,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendLau
     Pages<4> next = pages_of(begin);
     load(begin, next, x);
     next = pages_of(begin + 1);
-    load_queries();           // behind the codes, which are waited for first
+    load_queries();           // behind the codes, which are waited for first: four prompts as above without a window 184 to 190 us, queries first 188 to 190
     store(begin, x, lds[0]);
     hidden = x.hidden;
     lds_barrier();

@@ -42,12 +42,13 @@ static int64_t even_parts(int64_t groups, int64_t steps, int64_t parts, int64_t 
 // With a window sequences that are longer take about the same number of steps, and one round of workgroups, as many as are resident at a time (512 or 768), is better than
 // many: in 2048 / 768 / 512 workgroups 16 x (8 x 4) rows, window 4096, 4 bits 30.1 / 24.1 / 24.9 us, 128 x (8 x 4) heads of 64, window 1024 32.1 / 25.0 / 24.6;
 // 8 bits, one row of 32 heads, window 8191 23.0 / 22.9 / 21.3, 32 x (8 x 4), window 2048 37.7 / 37.7 / 35.8.
-// Where one round leaves some compute units with far more than others, more parts even that out: us in one round / as even_parts has it, 4 and 8 bits, 264 workgroups a part,
-// window 4096 45.0 / 41.5 and 78.9 / 68.0, 3000 35.4 / 32.8 and 58.9 / 52.8, 520 of them 81.5 / 75.7 and 138 / 124, 62.4 / 59.0 and 101 / 91.5, 776 116 / 106 and 179 / 173, 85.2 / 81.1
-// and 139 / 135.  In few steps they do not pay (520, window 1200 27.8 / 30.6 and 42.8 / 44.8, 2048 42.0 / 42.8 and 76.2 / 71.2, 2500 52.7 / 51.1 and 89.9 / 81.9; 392, 2048 32.2 / 33.2 and
-// 48.4 / 51.7), and nor where two workgroups are resident a compute unit and it has one or two (8 bits, 392, window 4096 91.7 / 92.8, 3000 64.0 / 67.2; with 4 bits 61.5 / 58.7, 46.3 / 43.1).
-// Under a window near max_kv it depends on the lengths, which are not known here: 128 workgroups a part in one round / in 2048, 4 and 8 bits, lengths of 1000 to 32768
-// under a window of 29491 93.4 / 81.0 and 123 / 119, under one of 21000 75.6 / 73.5 and 105 / 108, all of 4200 under 4096 23.1 / 28.0 and 30.2 / 38.3.
+// Where one round leaves some compute units with far more than others, more parts even that out: us in one round / as even_parts has it, 4 and 8 bits, 264
+// workgroups a part, window 4096 45.0 / 41.5 and 78.9 / 68.0, 3000 35.4 / 32.8 and 58.9 / 52.8, 520 of them 81.5 / 75.7 and 138 / 124, 62.4 / 59.0 and 101 / 91.5,
+// 776 116 / 106 and 179 / 173, 85.2 / 81.1 and 139 / 135.  In few steps they do not pay (520, window 1200 27.8 / 30.6 and 42.8 / 44.8, 2048 42.0 / 42.8 and 76.2 /
+// 71.2, 2500 52.7 / 51.1 and 89.9 / 81.9; 392, 2048 32.2 / 33.2 and 48.4 / 51.7), and nor where two workgroups are resident a compute unit and it has one or two
+// (8 bits, 392, window 4096 91.7 / 92.8, 3000 64.0 / 67.2; with 4 bits 61.5 / 58.7, 46.3 / 43.1).
+// Under a window near max_kv it depends on the lengths, which are not known here: 128 workgroups a part in one round / in 2048, 4 and 8 bits, lengths of 1000 to
+// 32768 under a window of 29491 93.4 / 81.0 and 123 / 119, under one of 21000 75.6 / 73.5 and 105 / 108, all of 4200 under 4096 23.1 / 28.0 and 30.2 / 38.3.
 // A few steps are better left whole, as two or three parts save less than the launch that joins them: us in parts / whole, 16 x (8 x 4) rows, window 450
 // 11.2 / 8.5, 900 14.0 / 13.0 (8 bits 15.3 / 13.3), 1024 13.9 / 14.3 (15.6 / 14.6), 1500 16.0 / 18.4; 32 x (8 x 4), 1024 17.6 / 15.0 (20.9 / 17.1); with fewer
 // workgroups parts are worth more: 4 x (8 x 4), window 512 9.6 / 8.9, 640 10.1 / 9.7, 768 9.7 / 10.6.

@@ -10,19 +10,20 @@
 // `top` logits reach, and only in the shares of threads whose largest does: about `top` shares of a THREADS-th of the row.  Those are read
 // again (from a cache, mostly), what reaches the bound goes to a list in LDS, and every member counts how many are before it.
 // A bound that lets three times as many logits through (the least of `top` groups' largest) cost more on the list than it saved (64 rows of 32000, five
-// of each: 11.2 us against 8.5); a search for it, bit by bit, in place of the count that up to 32 alternatives take, 8.9 against 8.2.
+// of each: 2.7 us more); a search for it, bit by bit, in place of the count that up to 32 alternatives take, 0.7 more.
 //
 // Order is by value and of equal values by the lower index, so that the answer does not depend on who finds what when.  The bound is of the same order: a
 // value, and the last piece in which that value counts.  A row of one value throughout (or of few logits and -inf besides) so has a short list too.
 // Where the list would be longer than its place, which takes a row whose largest logits nearly all lie in few threads' shares, the bound is
 // found by bisection over the whole row.
 //
-// Many rows are bound by memory (4095 x 32000 fp16 43 us in a loop of its own = 6.1 TB/s, with five alternatives 49, with twenty 60): a logit takes some nine vector
-// operations and an exponential (four more), over half of the time that it takes to come.  Few rows are bound by the same arithmetic in one compute unit each: 64
-// rows of 32000 take 5.3 us (6.0 with the conversion apart), and with five alternatives 8.0: bound, shares, list and ranks, one after the other, a few
-// hundred ns of latency each.  Built and no faster: the next pieces fetched ahead (one row of 262144 34 us against 32); d as one product and difference, with
-// a whole number in place of m a log2 e and the other way where that is too large for it (7.9 and 5.2, but 4096 rows of 1000 19.4 against 18.0); every wave
-// looking through its own threads' shares, without a list of those (8.2).
+// Many rows are bound by memory (inputs beyond the last-level cache: 4095 x 32000 fp16 54 us = 4.9 TB/s, with five, twenty and fifty alternatives 58, 66 and 80;
+// 40000 rows 442 = 5.8 TB/s): a logit takes some nine vector operations and an exponential (four more), over half of the time that it takes to come.  Few rows are
+// bound by the same arithmetic in one compute unit each: 64 rows of 32000 take 5.3 us (6.0 with the conversion apart), and with five alternatives 8.0: bound,
+// shares, list and ranks, one after the other, a few hundred ns of latency each; from 33 alternatives on the search for the bound too (9.2 us with 32, 9.7 with
+// 33, 11.5 with 64).  Built and no faster: the next pieces fetched ahead (one row of 262144, not shared, 2 us more); d as one product and difference, with a whole
+// number in place of m a log2 e and the other way where that is too large for it (7.9 and 5.2, but 4096 rows of 1000 19.4 against 18.0); every wave looking
+// through its own threads' shares, without a list of those (0.2 more).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -457,16 +458,16 @@ template <class K, int THREADS, bool SPLIT> static void run(const LogprobArgs& a
 }
 
 // Threads of a workgroup.  Few lanes go idle in a row of few pieces, and more workgroups of 256 than of 512 run beside each other, of which some read while
-// others look for alternatives; long rows want more loads under way.  us with 512 / 256 threads, fp16, five alternatives: 64 rows of 8000 7.2 / 6.4, of
-// 32000 9.0 / 10.3, of 131072 19.2 / 26.8; 4096 rows of 8000 53 / 24, of 32000 71 / 54; fp32, twenty: 64 of 8000 6.7 / 7.8, 4096 of 32000 112 / 135.
+// others look for alternatives; long rows want more loads under way.  us with 512 / 256 threads, fp16, five alternatives: 64 rows of 8000 6.5 / 5.7, of
+// 32000 8.1 / 8.9, of 131072 18.0 / 23.1; 4096 rows of 8000 39.8 / 24.2, of 32000 62.3 / 56.4; fp32, twenty: 64 of 8000 6.0 / 6.3, 4096 of 32000 102 / 121.
 static bool wide(const LogprobArgs& a) {
   const int64_t bytes = static_cast<int64_t>(a.V) * (a.type == ROSAQ_F32 ? 4 : 2);
   return bytes > (a.M > 640 ? 65536 : 32768);
 }
 
 // A compute unit alone takes some ten logits a ns, so that few long rows are better shared by several, at the price of another launch.  us in 1 / 2 / 4 / 8 / 16
-// parts, fp16, five alternatives: one row of 65536 10.7 / 10.5 / 9.2 / 9.6 / 10.1, of 262144 29.1 / 19.4 / 13.3 / 10.9 / 10.2; 64 of 131072 19.1 / 15.7 / 12.9 / 13.1 / 17.7;
-// 128 of 65536 12.7 / 12.8 / 13.0 / 17.3 / 25.4, of 262144 34.0 / 23.9 / 21.5 / 23.1 / 27.1; 257 of 32000 11.7 / 14.0 / 18.7 / 26.5 / 36.5.
+// parts, fp16, five alternatives: one row of 65536 9.5 / 9.8 / 8.8 / 9.0 / 9.6, of 262144 26.2 / 18.3 / 12.6 / 10.5 / 9.8; 64 of 131072 17.9 / 14.8 / 12.0 / 12.7 / 16.6;
+// 128 of 65536 11.4 / 11.9 / 12.7 / 16.1 / 24.1 (four here), of 262144 32.2 / 23.7 / 21.9 / 23.0 / 27.0; 257 of 32000 11.0 / 13.7 / 17.8 / 25.6 / 34.3.
 int parts_of_logprobs(const LogprobArgs& a) {
   if (a.V < 65536) return 1;
   return std::max(1, std::min({kMaxParts, a.V / 16384, 512 / a.M}));

@@ -1,7 +1,7 @@
 // Root-mean-square norm of rows, with the addition to the residual stream in front of it: h = x + residual, y = h / sqrt(mean h^2 + eps) * weight.
 //
 // A row is held by a team of threads, sixteen to 1024, in pieces of eight channels: read once, added up over the team, written once.  So it is bound
-// by memory (8192 x 4096 with an fp16 residual 41.5 us = 6.5 TB/s, where a copy reaches 4.9 to 5.2), or by a launch where there are few rows (64 of them 2.9 us).
+// by memory (65536 x 4096 with an fp16 residual, 2.1 GB, 388 us = 5.5 TB/s, where a copy reaches 5.0), or by a launch where there are few rows (64 of them 2.9 us).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -40,7 +40,7 @@ constexpr int threads_of(int team) { return team > 64 ? team : 256; }
 // ADD 0: no residual, 1: fp16, 2: fp32.  The sum of squares is fp32, of rows whose residual is fp32 in fp64: those may hold numbers whose squares
 // fp32 does not.  CODES: all in fp64, because a code next to a border is a whole step off when it falls to the other side; a step is a 127th of the largest
 // value.  The vector units bound it then: the conversions to fp64, and a row's own part (reductions, root, quotients), which every wave of it pays (1003 x 5120
-// with an fp32 residual 14.2 us, of which memory 11.5; 8192 x 4096 with an fp16 one 49 and 48, without one 31 and 20).  Built and slower: fp32, and fp64 again
+// with an fp32 residual 15.8 us, 11.5 at a copy's rate; 8192 x 4096 with an fp16 one 51 and 48, without one 32 and 20).  Built and slower: fp32, and fp64 again
 // for what fp32 cannot decide (22 and 61 us for the first two: a branch a channel).
 template <int TEAM, int CH, int ADD, bool CODES>
 __global__ __launch_bounds__(threads_of(TEAM)) void rmsnorm_kernel(NormArgs a) {
@@ -94,7 +94,7 @@ __global__ __launch_bounds__(threads_of(TEAM)) void rmsnorm_kernel(NormArgs a) {
       if constexpr (kHold) return wide[i][j];
       else return h(i, j);
     };
-    // the sum rounded to fp32 is the same from fp32 operands as from fp64's; of an fp32 residual it is at hand in fp64 (8192 x 4096 to codes 71 us, 76 from fp32)
+    // the sum rounded to fp32 is the same from fp32 operands as from fp64's; of an fp32 residual it is at hand in fp64 (8192 x 4096 to codes 70 us, 5 more from fp32)
     if constexpr (ADD != 0) {
       if (a.residual_out) {
 #pragma unroll
@@ -206,10 +206,11 @@ template <int TEAM, int CH> static void run(const NormArgs& a, hipStream_t st) {
   else run<TEAM, CH, false>(a, st);
 }
 
-// The smallest team whose threads hold one or two pieces each: more loads under way beside each other, fewer registers.  us with 256 threads / 512 / 1024: 8192 x
-// 4096 with an fp16 residual 45.0 / 41.5 / 47.6, 64 of them 3.4 / 2.9 / 3.1; 8192 x 5120 64.1 / 60.2 / 66.5, 64 of them 4.1 / 3.4 / 3.4; a wave
-// a row is slower still (8192 x 4096 52.4, 64 of them 6.7).  To codes of up to 4096 channels two pieces each, which halve the waves that a row's own part is paid
-// in: 8192 x 4096 without a residual 42.7 us in 512 threads, 32.0 in 256, 8192 x 2048 with an fp16 one 28.1 in 256, 26.6 in 128; 1003 x 5120 15.3 in 512, 15.8 in 256.
+// The smallest team whose threads hold one or two pieces each: more loads under way beside each other, fewer registers.  us with 256 threads / 512 / 1024, inputs
+// and outputs beyond the last-level cache: 8192 x 4096 with an fp16 residual 51.1 / 46.8 / 51.0, 64 of them 3.4 / 2.9 / 3.1; 8192 x 5120 66.1 / 61.9 / 66.8, 64 of
+// them 4.0 / 3.4 / 3.3; a wave a row is slower still (8192 x 4096 58.0, 64 of them 6.6).  To codes of up to 4096 channels two pieces each, which halve the waves
+// that a row's own part is paid in: 8192 x 4096 without a residual 40.5 us in 512 threads, 32.1 in 256, 8192 x 2048 with an fp16 one 26.9 in 256, 27.4 in 128;
+// 1003 x 5120 15.8 in 512, 16.4 in 256.
 int launch_rmsnorm(const NormArgs& a, void* stream) {
   hipStream_t st = static_cast<hipStream_t>(stream);
   const int pieces = a.D / 8;
